@@ -26,6 +26,8 @@
  *     compute units, the address of the static scratch array); with profiling off, calls
  *     from several host threads may run at once if each has its own workspace, outputs and
  *     stream.  Work runs on the device that is current when the call is made.
+ *   - The operators around the layer (switch_linear, switch_dropout, switch_balance_loss; at the
+ *     end of this file) follow the same rules; what they add is said with each.
  *   - An empty batch (T = 0) is legal: forward writes expert_counts = 0 and
  *     aux_loss = 0 (both fractions of Eq. 4 are empty sums), backward writes
  *     zeros to dW_r, db_r, dW_in, dW_out; the per-token arguments and the
@@ -66,14 +68,14 @@ typedef enum { SW_FFN_RELU = 0, SW_FFN_GEGLU = 1 } sw_ffn_kind;
 typedef enum {
     SW_OK = 0,
     SW_ERR_NULL = -1,      /* a required pointer is NULL                         */
-    SW_ERR_SHAPE = -2,     /* T, d_model, d_ff, E, n_groups out of range; rows not whole
+    SW_ERR_SHAPE = -2,     /* T, d_model, d_ff, E, n_groups (or M, K, N, n, k) out of range; rows not whole
                               16-byte chunks; bf16: an expert's weight matrix or its
                               slots x max(d_model, d_ff) activations reach 2 GB       */
     SW_ERR_VALUE = -3,     /* capacity_factor not finite or <= 0, alpha not finite,
                               expert_dropout or jitter_eps outside [0, 1), ntlb_rounds
                               outside 0 .. 16, unknown bits in flags                */
     SW_ERR_DTYPE = -4,     /* act_dtype is neither SW_F32 nor SW_BF16, or ffn_kind
-                              is not a sw_ffn_kind                               */
+                              is not a sw_ffn_kind, activation not a sw_activation */
     SW_ERR_WORKSPACE = -5, /* workspace NULL, misaligned or too small            */
     SW_ERR_ALIGN = -6,     /* a tensor pointer is not 16-byte aligned            */
     SW_ERR_LAUNCH = -7,    /* the HIP runtime refused a launch (see hipGetLastError) */
@@ -234,6 +236,125 @@ int switch_forward_static(const switch_config *cfg, const void *x, const float *
                           void *y, int32_t *expert_index, float *gate,
                           int32_t *position_in_expert, uint8_t *dropped, int32_t *expert_counts,
                           float *aux_loss, float *router_logits /* or NULL */, void *hip_stream);
+
+/* ==== Operators around the layer ==========================================================
+ * In the models of the paper every other feed-forward sublayer is dense, every sublayer's
+ * output passes dropout on its way into the residual stream, and a router of the caller's own
+ * (several choices per token, padded batches) needs the balance loss by itself.
+ */
+
+/* Activation of switch_linear.  SW_ACT_GELU: u Phi(u), exact.  SW_ACT_GEGLU: GELU(u) * v with W
+ * [K, 2 N] and bias [2 N], the N gate columns u first and the N linear columns v after them. */
+typedef enum { SW_ACT_NONE = 0, SW_ACT_RELU = 1, SW_ACT_GELU = 2, SW_ACT_GEGLU = 3 } sw_activation;
+
+typedef struct {
+    int64_t M;               /* rows of x (0 .. 2^31 - 1)                             */
+    int64_t K;               /* columns of x, rows of W                               */
+    int64_t N;               /* columns of y.  K, N: whole 16-byte chunks (multiples of 8 for SW_BF16,
+                                of 4 for SW_F32); K and the columns of W below 2^21, W below 2 GB */
+    int32_t act_dtype;       /* sw_dtype of x, W, residual, y, z, dy, dx, dW          */
+    int32_t activation;      /* sw_activation                                         */
+    float dropout;           /* rate in [0, 1), rounded down to a multiple of 2^-16; 0: off */
+    int32_t flags;           /* 0                                                     */
+    uint64_t seed;           /* of the dropout; the same in forward and backward      */
+} switch_linear_config;
+
+/* Bytes of device workspace of switch_linear (backward = 0) or of switch_linear_backward
+ * (backward = 1); may be 0.  Host only.  The workspace must be 256-byte aligned.  It holds nothing
+ * between calls: calls on one stream may share it, calls (and captured graphs) that may run at the
+ * same time may not. */
+int switch_linear_workspace_size(const switch_linear_config *cfg, int backward, size_t *bytes_out /* host */);
+
+/*
+ * One product with its epilogue:
+ *   z = x W + bias        [M, N], for SW_ACT_GEGLU [M, 2 N]
+ *   y = residual + dropout(act(z))
+ * Products are summed in fp32, the epilogue is fp32 throughout; y and z are rounded once.  The
+ * dropout mask is switch_dropout's for the same rate and seed and a tensor of M * N elements.
+ * z, where asked for, is what switch_linear_backward needs; nothing else is kept.  residual and y
+ * may be the same tensor; other tensors must not overlap an output.  M = 0: nothing is done (pointers may be NULL).
+ */
+int switch_linear(const switch_linear_config *cfg,
+                  const void *x,          /* [M, K]   act_dtype                        */
+                  const void *W,          /* [K, N]   act_dtype ([K, 2 N] for SW_ACT_GEGLU) */
+                  const float *bias,      /* [columns of W] fp32, or NULL              */
+                  const void *residual,   /* [M, N]   act_dtype, or NULL               */
+                  void *y,                /* [M, N]   act_dtype (out)                  */
+                  void *z,                /* [M, columns of W] act_dtype (out), or NULL */
+                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradients of L = <dy, y>:  dz = act'(z) * dropout(dy),  dx = dz W^T,  dW = x^T dz,
+ * db = sum of dz's rows (ReLU'(0) = 0); the residual's gradient is dy itself.  Each of dx, dW, db may
+ * be NULL, not all.  z: from switch_linear with the same cfg; not read (may be NULL) for
+ * SW_ACT_NONE.  W is read only for dx, x only for dW; the other may be NULL.  With SW_BF16, SW_ACT_GELU
+ * and SW_ACT_GEGLU round dz to bf16 for the two products (db sums it in fp32); the others need no
+ * rounding: the dropout scale is applied to the sums.  M = 0: dW and db are zeros.
+ */
+int switch_linear_backward(const switch_linear_config *cfg,
+                           const void *dy,   /* [M, N] act_dtype                       */
+                           const void *x, const void *W, const void *z,
+                           void *dx,         /* [M, K] act_dtype (out), or NULL        */
+                           void *dW,         /* W's shape, act_dtype (out), or NULL    */
+                           float *db,        /* [columns of W] fp32 (out), or NULL     */
+                           void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * y_i = residual_i + dropout(x_i), n elements of any shape (0 <= n < 2^40).  Element i is drawn with the library's
+ * generator ("Random draws" above), stream s = 3, as the expert dropout's hidden unit i: two
+ * elements a draw, but i / 2 is taken to 64 bits: its low half is idx, and its high half times
+ * 0x632BE5AB is added to seed_hi.  The mask is never stored.  Backward: the residual's gradient
+ * is dy, that of x is this function of dy with the same rate and seed (another gradient of x may
+ * be handed in as residual).  y may be x or residual; otherwise it must not overlap them.  residual
+ * may be NULL.  Sums in fp32, rounded once.
+ */
+int switch_dropout(int64_t n, int32_t act_dtype, float rate, uint64_t seed,
+                   const void *x, const void *residual /* or NULL */, void *y, void *hip_stream);
+
+typedef struct {
+    int64_t T;               /* tokens (0 .. 2^31 - 1)                                */
+    int64_t E;               /* experts (1 .. 4096)                                   */
+    int64_t k;               /* choices per token (1 .. E); T * k < 2^31              */
+    int64_t n_groups;        /* routing groups as in switch_config (0 is read as 1, at most 65535) */
+    float alpha;             /* coefficient of the loss                               */
+    int32_t flags;           /* 0                                                     */
+} switch_balance_config;
+
+/* Bytes of device workspace of switch_balance_loss.  Host only; rules as for switch_linear. */
+int switch_balance_workspace_size(const switch_balance_config *cfg, size_t *bytes_out /* host */);
+
+/*
+ * The balance loss (Eqs. 4-6) of any router's logits and choices, with padding:
+ *   p = softmax of each row of logits (fp32)
+ *   per group: n = tokens with token_mask != 0 (all, if it is NULL), P_i = sum p_i / n over them,
+ *   f_i = expert_counts_i / (n k), expert_counts_i = their choices of expert i
+ *   loss = alpha * E * mean over the groups of sum_i f_i P_i      (a group without tokens adds 0)
+ * Rows with token_mask = 0 are not read, whatever they hold.  Choices outside 0 .. E - 1 are not
+ * counted; an expert named twice by a token counts twice.  A logit may be -inf (an expert that the
+ * token may not choose); a row of nothing else has p = 0.  Sums in a fixed order: the same inputs
+ * give the same bits.
+ */
+int switch_balance_loss(const switch_balance_config *cfg,
+                        const float *logits,          /* [T, E]                            */
+                        const int32_t *expert_index,  /* [T, k]                            */
+                        const uint8_t *token_mask,    /* [T] or NULL                       */
+                        float *loss,                  /* [1] (out)                         */
+                        int32_t *expert_counts,       /* [n_groups, E] (out)               */
+                        int32_t *token_counts,        /* [n_groups] (out) n of each group  */
+                        void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * dlogits of d_loss * loss, the counts held constant (f is not differentiable):
+ *   dlogits_j = p_j (c_j - sum_i p_i c_i),  c_i = d_loss * alpha * E * f_i / (n_groups n)
+ * Masked rows and rows of -inf get zeros.  expert_counts and token_counts are switch_balance_loss's.
+ * dlogits may be logits' own memory; otherwise they must not overlap.
+ */
+int switch_balance_loss_backward(const switch_balance_config *cfg,
+                                 float d_loss,        /* host scalar                       */
+                                 const float *logits, const uint8_t *token_mask /* or NULL */,
+                                 const int32_t *expert_counts, const int32_t *token_counts,
+                                 float *dlogits,      /* [T, E] (out)                      */
+                                 void *hip_stream);
 
 /* Human-readable name of a status code.  Host; static storage. */
 const char *switch_status_string(int status);

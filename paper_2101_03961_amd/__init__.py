@@ -6,16 +6,29 @@ kernels of ``libswitchffn.so``.  There is no CPU or PyTorch fallback: if the
 library is missing or cannot be loaded, importing the binding raises.
 """
 from .binding import (  # noqa: F401
+    SW_ACT_GEGLU,
+    SW_ACT_GELU,
+    SW_ACT_NONE,
+    SW_ACT_RELU,
     SW_BF16,
     SW_F32,
     SW_FFN_GEGLU,
     SW_FFN_RELU,
     SW_FLAG_FUSED_DISPATCH,
+    SwitchBalanceConfig,
     SwitchConfig,
     SwitchError,
+    SwitchLinearConfig,
     library_path,
     switch_backward,
+    switch_balance_loss,
+    switch_balance_loss_backward,
+    switch_balance_workspace_size,
     switch_capacity,
+    switch_dropout,
+    switch_linear,
+    switch_linear_backward,
+    switch_linear_workspace_size,
     SW_STATIC_SCRATCH_BYTES,
     switch_forward,
     switch_forward_static,

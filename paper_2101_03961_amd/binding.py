@@ -11,6 +11,7 @@ _LIB_PATH = os.path.join(HERE, "libswitchffn.so")
 SW_F32, SW_BF16 = 0, 1
 SW_FFN_RELU, SW_FFN_GEGLU = 0, 1
 SW_FLAG_FUSED_DISPATCH = 1
+SW_ACT_NONE, SW_ACT_RELU, SW_ACT_GELU, SW_ACT_GEGLU = 0, 1, 2, 3
 
 
 class SwitchError(RuntimeError):
@@ -35,6 +36,32 @@ class SwitchConfig(ctypes.Structure):
         ("jitter_eps", ctypes.c_float),
         ("seed", ctypes.c_uint64),
         ("ntlb_rounds", ctypes.c_int32),
+        ("flags", ctypes.c_int32),
+    ]
+
+
+class SwitchLinearConfig(ctypes.Structure):
+    """Mirror of the C struct switch_linear_config."""
+    _fields_ = [
+        ("M", ctypes.c_int64),
+        ("K", ctypes.c_int64),
+        ("N", ctypes.c_int64),
+        ("act_dtype", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+        ("dropout", ctypes.c_float),
+        ("flags", ctypes.c_int32),
+        ("seed", ctypes.c_uint64),
+    ]
+
+
+class SwitchBalanceConfig(ctypes.Structure):
+    """Mirror of the C struct switch_balance_config."""
+    _fields_ = [
+        ("T", ctypes.c_int64),
+        ("E", ctypes.c_int64),
+        ("k", ctypes.c_int64),
+        ("n_groups", ctypes.c_int64),
+        ("alpha", ctypes.c_float),
         ("flags", ctypes.c_int32),
     ]
 
@@ -66,6 +93,18 @@ def _load():
     lib.switch_forward_static.argtypes = [cfgp] + [vp] * 13 + [vp]
     lib.switch_backward.restype = ctypes.c_int
     lib.switch_backward.argtypes = [cfgp, vp, ctypes.c_float] + [vp] * 10 + [vp, ctypes.c_size_t, vp]
+    lincfgp, balcfgp = ctypes.POINTER(SwitchLinearConfig), ctypes.POINTER(SwitchBalanceConfig)
+    sizep = ctypes.POINTER(ctypes.c_size_t)
+    for name, argtypes in (
+            ("switch_linear_workspace_size", [lincfgp, ctypes.c_int, sizep]),
+            ("switch_linear", [lincfgp] + [vp] * 6 + [vp, ctypes.c_size_t, vp]),
+            ("switch_linear_backward", [lincfgp] + [vp] * 7 + [vp, ctypes.c_size_t, vp]),
+            ("switch_dropout", [ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_uint64] + [vp] * 4),
+            ("switch_balance_workspace_size", [balcfgp, sizep]),
+            ("switch_balance_loss", [balcfgp] + [vp] * 6 + [vp, ctypes.c_size_t, vp]),
+            ("switch_balance_loss_backward", [balcfgp, ctypes.c_float] + [vp] * 6)):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = argtypes
     lib.switch_status_string.restype = ctypes.c_char_p
     lib.switch_status_string.argtypes = [ctypes.c_int]
     lib.switch_profile_enable.restype = ctypes.c_int
@@ -148,6 +187,69 @@ def switch_backward(cfg: SwitchConfig, dy, d_aux: float, x, W_r, b_r, W_in, W_ou
                                  hip_stream or None)
     if check and st != 0:
         raise SwitchError(st, "switch_backward")
+    return st
+
+
+def switch_linear_workspace_size(cfg: SwitchLinearConfig, backward: bool) -> int:
+    out = ctypes.c_size_t(0)
+    st = _load().switch_linear_workspace_size(ctypes.byref(cfg), 1 if backward else 0, ctypes.byref(out))
+    if st != 0:
+        raise SwitchError(st, "switch_linear_workspace_size")
+    return out.value
+
+
+def switch_linear(cfg: SwitchLinearConfig, x, W, bias, residual, y, z, workspace, workspace_bytes: int,
+                  hip_stream: int = 0, check: bool = True) -> int:
+    st = _load().switch_linear(ctypes.byref(cfg), _p(x), _p(W), _p(bias), _p(residual), _p(y), _p(z),
+                               _p(workspace), int(workspace_bytes), hip_stream or None)
+    if check and st != 0:
+        raise SwitchError(st, "switch_linear")
+    return st
+
+
+def switch_linear_backward(cfg: SwitchLinearConfig, dy, x, W, z, dx, dW, db, workspace,
+                           workspace_bytes: int, hip_stream: int = 0, check: bool = True) -> int:
+    st = _load().switch_linear_backward(ctypes.byref(cfg), _p(dy), _p(x), _p(W), _p(z), _p(dx), _p(dW),
+                                        _p(db), _p(workspace), int(workspace_bytes), hip_stream or None)
+    if check and st != 0:
+        raise SwitchError(st, "switch_linear_backward")
+    return st
+
+
+def switch_dropout(n: int, act_dtype: int, rate: float, seed: int, x, residual, y, hip_stream: int = 0,
+                   check: bool = True) -> int:
+    st = _load().switch_dropout(n, act_dtype, rate, seed, _p(x), _p(residual), _p(y), hip_stream or None)
+    if check and st != 0:
+        raise SwitchError(st, "switch_dropout")
+    return st
+
+
+def switch_balance_workspace_size(cfg: SwitchBalanceConfig) -> int:
+    out = ctypes.c_size_t(0)
+    st = _load().switch_balance_workspace_size(ctypes.byref(cfg), ctypes.byref(out))
+    if st != 0:
+        raise SwitchError(st, "switch_balance_workspace_size")
+    return out.value
+
+
+def switch_balance_loss(cfg: SwitchBalanceConfig, logits, expert_index, token_mask, loss, expert_counts,
+                        token_counts, workspace, workspace_bytes: int, hip_stream: int = 0,
+                        check: bool = True) -> int:
+    st = _load().switch_balance_loss(ctypes.byref(cfg), _p(logits), _p(expert_index), _p(token_mask),
+                                     _p(loss), _p(expert_counts), _p(token_counts), _p(workspace),
+                                     int(workspace_bytes), hip_stream or None)
+    if check and st != 0:
+        raise SwitchError(st, "switch_balance_loss")
+    return st
+
+
+def switch_balance_loss_backward(cfg: SwitchBalanceConfig, d_loss: float, logits, token_mask, expert_counts,
+                                 token_counts, dlogits, hip_stream: int = 0, check: bool = True) -> int:
+    st = _load().switch_balance_loss_backward(ctypes.byref(cfg), float(d_loss), _p(logits), _p(token_mask),
+                                              _p(expert_counts), _p(token_counts), _p(dlogits),
+                                              hip_stream or None)
+    if check and st != 0:
+        raise SwitchError(st, "switch_balance_loss_backward")
     return st
 
 

@@ -269,9 +269,20 @@ void prof_end(hipStream_t s) {
     g_open = -1;
 }
 
-static int status_of(hipError_t e) { return e == hipSuccess ? SW_OK : SW_ERR_LAUNCH; }
+// 4-byte words set to zero (stays valid under stream capture, unlike a memset node)
+__global__ __launch_bounds__(256) void fill_zero_kernel(uint32_t *__restrict__ p, size_t words) {
+    const size_t stride = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += stride) p[i] = 0u;
+}
 
-static bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+int fill_zero(void *p, size_t bytes, hipStream_t s) {
+    const size_t words = bytes / 4;
+    if (words == 0) return SW_OK;
+    size_t blocks = (words + 255) / 256;
+    if (blocks > 4096) blocks = 4096;
+    hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)blocks), dim3(256), 0, s, (uint32_t *)p, words);
+    return status_of(hipGetLastError());
+}
 
 }  // namespace sw
 
@@ -318,21 +329,6 @@ int switch_workspace_size(const switch_config *cfg, size_t *bytes_out) {
     if (st != SW_OK) return st;
     *bytes_out = layout_workspace(cfg).total;
     return SW_OK;
-}
-
-// 4-byte words set to zero (stays valid under stream capture, unlike a memset node)
-__global__ __launch_bounds__(256) void fill_zero_kernel(uint32_t *__restrict__ p, size_t words) {
-    const size_t stride = (size_t)gridDim.x * 256;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += stride) p[i] = 0u;
-}
-
-static int fill_zero(void *p, size_t bytes, hipStream_t s) {
-    const size_t words = bytes / 4;
-    if (words == 0) return SW_OK;
-    size_t blocks = (words + 255) / 256;
-    if (blocks > 4096) blocks = 4096;
-    hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)blocks), dim3(256), 0, s, (uint32_t *)p, words);
-    return status_of(hipGetLastError());
 }
 
 // The forward pass on a workspace that has been checked: argument checks, then launches only.
@@ -506,11 +502,11 @@ const char *switch_status_string(int status) {
     switch (status) {
     case SW_OK: return "ok";
     case SW_ERR_NULL: return "a required pointer is NULL";
-    case SW_ERR_SHAPE: return "shape out of range (T, E, d_model, d_ff; 16-byte row chunks)";
+    case SW_ERR_SHAPE: return "shape out of range (T, E, d_model, d_ff; M, K, N; n, k; 16-byte row chunks)";
     case SW_ERR_VALUE:
-        return "capacity_factor must be finite and > 0; alpha, d_aux finite; expert_dropout and "
+        return "capacity_factor must be finite and > 0; alpha, d_aux, d_loss finite; dropout rates and "
                "jitter_eps in [0, 1); ntlb_rounds in 0..16; flags: known bits only";
-    case SW_ERR_DTYPE: return "act_dtype must be SW_F32 or SW_BF16, ffn_kind SW_FFN_RELU or SW_FFN_GEGLU";
+    case SW_ERR_DTYPE: return "act_dtype must be SW_F32 or SW_BF16, ffn_kind a sw_ffn_kind, activation a sw_activation";
     case SW_ERR_WORKSPACE: return "workspace NULL, not 256-byte aligned, or too small";
     case SW_ERR_ALIGN: return "tensor pointer not 16-byte aligned";
     case SW_ERR_LAUNCH: return "HIP launch failed";

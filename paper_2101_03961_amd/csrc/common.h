@@ -221,6 +221,12 @@ struct ProfScope {
     ~ProfScope() { prof_end(s); }
 };
 
+// ---- host helpers of the entry points ------------------------------------------
+static inline int status_of(hipError_t e) { return e == hipSuccess ? SW_OK : SW_ERR_LAUNCH; }
+static inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+// whole 4-byte words; returns a sw_status
+int fill_zero(void *p, size_t bytes, hipStream_t s);
+
 struct RouterWgradArgs;   // router_wgrad.h
 
 // ---- kernel launchers (each returns hipSuccess or the launch error) ----------

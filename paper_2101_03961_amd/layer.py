@@ -1,8 +1,10 @@
-"""Buffer-owning convenience wrapper around the C ABI.
+"""Buffer-owning convenience wrappers around the C ABI.
 
 `SwitchLayer` allocates the output tensors and the workspace with torch (device
 memory and streams are all torch is used for) and forwards every call to
-`switch_forward` / `switch_backward`.  It performs no arithmetic.
+`switch_forward` / `switch_backward`; `SwitchLinear` and `SwitchBalanceLoss` do the same
+for the operators around the layer, `dropout` for the one without buffers.  They perform no
+arithmetic.
 """
 from __future__ import annotations
 
@@ -98,3 +100,138 @@ class SwitchLayer:
                           self._stream())
         return dict(dx=self.dx, dW_r=self.dW_r, db_r=self.db_r, dW_in=self.dW_in,
                     dW_out=self.dW_out)
+
+
+def _check(device, want) -> None:
+    """Tensors (or None where they may be left out) are what the kernels will read."""
+    for name, t, shape, dtype in want:
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous()
+                              or t.device != device):
+            raise ValueError("%s must be a contiguous %s tensor of shape %s on %s, got %s %s on %s"
+                             % (name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
+
+
+class SwitchLinear:
+    """y = residual + dropout(act(x W + bias)) and its gradients (switch_linear).
+
+    `train`: also keep z for the backward pass and allocate the gradients.  Outputs are the
+    object's own buffers, overwritten by the next call."""
+
+    ACTIVATIONS = {"none": B.SW_ACT_NONE, "relu": B.SW_ACT_RELU, "gelu": B.SW_ACT_GELU,
+                   "geglu": B.SW_ACT_GEGLU}
+
+    def __init__(self, M: int, K: int, N: int, activation: str = "none", dropout: float = 0.0, seed: int = 0,
+                 dtype: str = "bf16", device: str = "cuda:0", train: bool = False):
+        if not torch.cuda.is_available():
+            raise RuntimeError("SwitchLinear needs a GPU: the product runs only in the HIP library")
+        self.cfg = B.SwitchLinearConfig(M, K, N, B.SW_BF16 if dtype == "bf16" else B.SW_F32,
+                                        self.ACTIVATIONS[activation], float(dropout), 0, int(seed))
+        self.columns = N * (2 if activation == "geglu" else 1)   # of W
+        self.device = torch.device(device)
+        self.act = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.workspace_bytes = B.switch_linear_workspace_size(self.cfg, False)
+        if train:
+            self.workspace_bytes = max(self.workspace_bytes, B.switch_linear_workspace_size(self.cfg, True))
+        dev = self.device
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+        self.y = torch.empty((M, N), dtype=self.act, device=dev)
+        self.z = self.dx = self.dW = self.db = None
+        self.train = train
+        if train:
+            if activation != "none":
+                self.z = torch.empty((M, self.columns), dtype=self.act, device=dev)
+            self.dx = torch.empty((M, K), dtype=self.act, device=dev)
+            self.dW = torch.empty((K, self.columns), dtype=self.act, device=dev)
+            self.db = torch.empty(self.columns, dtype=torch.float32, device=dev)
+
+    def set_seed(self, seed: int) -> None:
+        """Seed of the dropout for the next forward + backward pair."""
+        self.cfg.seed = int(seed)
+
+    def _stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def forward(self, x, W, bias=None, residual=None) -> torch.Tensor:
+        c = self.cfg
+        _check(self.device, [("x", x, (c.M, c.K), self.act), ("W", W, (c.K, self.columns), self.act),
+                             ("bias", bias, (self.columns,), torch.float32),
+                             ("residual", residual, (c.M, c.N), self.act)])
+        with torch.cuda.device(self.device):
+            B.switch_linear(c, x, W, bias, residual, self.y, self.z, self.workspace, self.workspace_bytes,
+                            self._stream())
+        return self.y
+
+    def backward(self, dy, x, W, with_bias: bool = True) -> Dict[str, Optional[torch.Tensor]]:
+        """Gradients from dy and the z of the last forward pass; the residual's gradient is dy."""
+        if not self.train:
+            raise ValueError("backward needs SwitchLinear(..., train=True)")
+        c = self.cfg
+        _check(self.device, [("dy", dy, (c.M, c.N), self.act), ("x", x, (c.M, c.K), self.act),
+                             ("W", W, (c.K, self.columns), self.act)])
+        db = self.db if with_bias else None
+        with torch.cuda.device(self.device):
+            B.switch_linear_backward(c, dy, x, W, self.z, self.dx, self.dW, db, self.workspace,
+                                     self.workspace_bytes, self._stream())
+        return dict(dx=self.dx, dW=self.dW, db=db)
+
+
+def dropout(x, rate: float, seed: int, residual=None, out=None) -> torch.Tensor:
+    """residual + dropout(x) (switch_dropout); the gradient of x is the same call on that of the result."""
+    if x.dtype not in (torch.bfloat16, torch.float32) or x.device.type != "cuda":
+        raise ValueError("x must be a bfloat16 or float32 tensor on a GPU, got %s on %s" % (x.dtype, x.device))
+    shape = tuple(x.shape)
+    out = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    _check(x.device, [("x", x, shape, x.dtype), ("residual", residual, shape, x.dtype),
+                      ("out", out, shape, x.dtype)])
+    with torch.cuda.device(x.device):
+        B.switch_dropout(x.numel(), B.SW_BF16 if x.dtype == torch.bfloat16 else B.SW_F32, rate, int(seed), x,
+                         residual, out, torch.cuda.current_stream(x.device).cuda_stream)
+    return out
+
+
+class SwitchBalanceLoss:
+    """Balance loss, counts and gradient of the logits for a router of the caller's own
+    (switch_balance_loss).  Outputs are the object's own buffers."""
+
+    def __init__(self, T: int, E: int, k: int = 1, alpha: float = 0.01, n_groups: int = 1,
+                 device: str = "cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("SwitchBalanceLoss needs a GPU: the loss is computed only in the HIP library")
+        self.cfg = B.SwitchBalanceConfig(T, E, k, int(n_groups), float(alpha), 0)
+        self.device = torch.device(device)
+        self.workspace_bytes = B.switch_balance_workspace_size(self.cfg)
+        dev, groups = self.device, max(int(n_groups), 1)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)
+        self.loss = torch.empty(1, dtype=torch.float32, device=dev)
+        self.expert_counts = torch.empty((groups, E), dtype=torch.int32, device=dev)
+        self.token_counts = torch.empty(groups, dtype=torch.int32, device=dev)
+        self.dlogits = None
+
+    def _stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _check_inputs(self, logits, token_mask, expert_index=None) -> None:
+        c = self.cfg
+        _check(self.device, [("logits", logits, (c.T, c.E), torch.float32),
+                             ("expert_index", expert_index, (c.T, c.k), torch.int32),
+                             ("token_mask", token_mask, (c.T,), torch.uint8)])
+
+    def forward(self, logits, expert_index, token_mask=None) -> Dict[str, torch.Tensor]:
+        """expert_index [T, k] int32 ([T] for k = 1), token_mask [T] uint8: 0 = padding."""
+        if expert_index.dim() == 1:
+            expert_index = expert_index[:, None]
+        self._check_inputs(logits, token_mask, expert_index)
+        with torch.cuda.device(self.device):
+            B.switch_balance_loss(self.cfg, logits, expert_index, token_mask, self.loss, self.expert_counts,
+                                  self.token_counts, self.workspace, self.workspace_bytes, self._stream())
+        return dict(loss=self.loss, expert_counts=self.expert_counts, token_counts=self.token_counts)
+
+    def backward(self, logits, token_mask=None, d_loss: float = 1.0) -> torch.Tensor:
+        """Gradient of the logits, from the counts of the last forward pass."""
+        self._check_inputs(logits, token_mask)
+        if self.dlogits is None:
+            self.dlogits = torch.empty((self.cfg.T, self.cfg.E), dtype=torch.float32, device=self.device)
+        with torch.cuda.device(self.device):
+            B.switch_balance_loss_backward(self.cfg, d_loss, logits, token_mask, self.expert_counts,
+                                           self.token_counts, self.dlogits, self._stream())
+        return self.dlogits

@@ -1,0 +1,447 @@
+"""The operators around the layer against their definitions in 64 bits.
+
+Tolerances.  u = half a step of the storage type relative to the value (bf16 2^-8, fp32 2^-24) for each
+rounding to it.  A sum of n products in fp32, in whatever order, is off by at most (n + 2) 2^-24 of the sum
+of the products' magnitudes; its errors are independent in sign, so the norm of a whole output's error
+stays below (sqrt(n) + 8) 2^-24 of the norm of those magnitudes' root sum of squares -- taken here as the
+norm of the output, with which it grows for inputs of random sign; the 8 covers the epilogue's operations
+and the fit of the normal distribution function (1.5e-7).  Where dz is rounded to bf16 for the products of
+the backward pass, each product is off by another 2^-8 of itself.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2101_03961_amd as sw
+from paper_2101_03961_amd.layer import SwitchBalanceLoss, SwitchLayer, SwitchLinear, dropout
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+U32 = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+ACTS = ("none", "relu", "gelu", "geglu")
+
+
+def normal(gen, *size):
+    return torch.randn(size, generator=gen, dtype=torch.float64)
+
+
+def keep_factor(n, rate, seed, first=0):
+    """0 or 1 / (1 - rate) of elements first .. first + n - 1, from the header's definition, word by word."""
+    thr = math.floor(float(np.float32(rate)) * 65536)
+    i = np.arange(first, first + n, dtype=np.uint64)
+    pair = i >> np.uint64(1)
+    z = pair.astype(np.uint32) ^ np.uint32(seed & 0xFFFFFFFF)
+    z = z * np.uint32(0x9E3779B1)
+    z ^= z >> np.uint32(15)
+    term = ((seed >> 32) + 3 * 0x7F4A7C15) & 0xFFFFFFFF
+    z = (z + np.uint32(term) + (pair >> np.uint64(32)).astype(np.uint32) * np.uint32(0x632BE5AB)) * np.uint32(0x85EBCA77)
+    z ^= z >> np.uint32(13)
+    z = z * np.uint32(0xC2B2AE3D)
+    z ^= z >> np.uint32(16)
+    half = np.where(i & np.uint64(1), z >> np.uint32(16), z & np.uint32(0xFFFF))
+    return torch.from_numpy(np.where(half >= thr, 65536.0 / (65536.0 - thr), 0.0))
+
+
+def phi(u):
+    return 0.5 * torch.erfc(-u / math.sqrt(2.0))
+
+
+def act64(act, z):
+    if act == "geglu":
+        u, v = z.chunk(2, dim=1)
+        return u * phi(u) * v
+    return {"none": z, "relu": z.clamp(min=0.0), "gelu": z * phi(z)}[act]
+
+
+def dz64(act, z, g):
+    if act == "none":
+        return g
+    if act == "relu":
+        return g * (z > 0)
+    slope = lambda u: phi(u) + u * torch.exp(-u * u / 2) / math.sqrt(2 * math.pi)
+    if act == "gelu":
+        return g * slope(z)
+    u, v = z.chunk(2, dim=1)
+    return torch.cat((g * v * slope(u), g * u * phi(u)), dim=1)
+
+
+def linear_case(M, K, N, act, dtype, seed, bias=True, residual=True):
+    gen = torch.Generator().manual_seed(seed)
+    cols = N * (2 if act == "geglu" else 1)
+    dt = DT[dtype]
+    t = {"x": normal(gen, M, K).to(dt), "W": (normal(gen, K, cols) / math.sqrt(K)).to(dt),
+         "bias": normal(gen, cols).float() if bias else None,
+         "residual": normal(gen, M, N).to(dt) if residual else None, "dy": normal(gen, M, N).to(dt)}
+    dev = {k: None if v is None else v.to(DEV) for k, v in t.items()}
+    return {k: None if v is None else v.double() for k, v in t.items()}, dev
+
+
+def close(name, got, want, bound, norm):
+    """Each element within its bound, the whole within norm of the whole."""
+    got = got.detach().cpu().double()
+    assert got.shape == want.shape, name
+    assert torch.isfinite(got).all(), name
+    err = (got - want).abs()
+    worst = (err - bound).max().item() if err.numel() else 0.0
+    assert worst <= 0.0, (name, "element off by %g over its bound" % worst)
+    total = float(torch.linalg.norm(err)) / max(float(torch.linalg.norm(want)), 1e-300)
+    assert total <= norm, (name, "norm", total, norm)
+
+
+SIZES = [(1, 64, 128), (1, 8, 8), (3, 768, 2048), (16, 520, 136), (17, 200, 1000), (33, 1024, 264), (64, 264, 64),
+         (65, 136, 520), (129, 72, 392), (255, 1000, 200), (300, 64, 24), (513, 328, 776), (1025, 256, 256)]
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_linear_forward_and_backward(M, K, N, dtype, act):
+    rate = (0.0, 0.1)[(M + K) % 2 == 0 or act == "none"]
+    seed = 0x123456789ABCDEF + M
+    ref, dev = linear_case(M, K, N, act, dtype, seed=M * 7 + K, bias=M % 2 == 1, residual=N % 16 == 8)
+    op = SwitchLinear(M, K, N, act, rate, seed, dtype, DEV, train=True)
+    u = U[dtype]
+    for t in (op.y, op.dx, op.dW, op.db) + (() if op.z is None else (op.z,)):
+        t.fill_(float("nan"))   # everything is written
+    y = op.forward(dev["x"], dev["W"], dev["bias"], dev["residual"])
+    grads = op.backward(dev["dy"], dev["x"], dev["W"])
+    torch.cuda.synchronize()
+    # forward
+    z = ref["x"] @ ref["W"]
+    mag = ref["x"].abs() @ ref["W"].abs()
+    if ref["bias"] is not None:
+        z, mag = z + ref["bias"], mag + ref["bias"].abs()
+    ez = (K + 2) * U32 * mag
+    factor = keep_factor(M * N, rate, seed).reshape(M, N)
+    want = act64(act, z)
+    if act == "geglu":
+        zu, zv = z.chunk(2, dim=1)
+        eu, ev = ez.chunk(2, dim=1)
+        ea = zv.abs() * (1.13 * eu + 2e-7 * zu.abs()) + want.abs() / zv.abs().clamp(min=1e-30) * ev + 1.13 * eu * ev
+    elif act == "gelu":
+        ea = 1.13 * ez + 2e-7 * z.abs()
+    else:
+        ea = ez
+    want, ea = want * factor, (ea + 4 * U32 * want.abs()) * factor
+    if ref["residual"] is not None:
+        want, ea = want + ref["residual"], ea + U32 * (want.abs() + ref["residual"].abs())
+    norm = (math.sqrt(K) + 8) * U32 + (u if dtype == "bf16" else U32)
+    close("y", y, want, u * (want.abs() + ea) + ea, norm)
+    if op.z is not None:
+        close("z", op.z, z, u * (z.abs() + ez) + ez, norm)
+        z = op.z.cpu().double()   # what the backward pass is given
+    # backward
+    g = ref["dy"] * factor
+    dz = dz64(act, z, g)
+    # (the fit of the normal distribution function, per dz; its rounding for the products)
+    edz = dz.abs() * 8 * U32
+    if act in ("gelu", "geglu"):
+        edz = edz + 4e-7 * (torch.cat((g * z.chunk(2, 1)[1], g * z.chunk(2, 1)[0]), 1).abs() * (1 + z.abs()) if act == "geglu"
+                            else g.abs() * (1 + z.abs()))
+    close("db", grads["db"], dz.sum(0), edz.sum(0) + (M + 2) * U32 * dz.abs().sum(0),
+          (math.sqrt(M) + 16) * U32 * max(1.0, float(torch.linalg.norm(dz) / torch.linalg.norm(dz.sum(0)))))
+    rounded = u if dtype == "bf16" and act in ("gelu", "geglu") else 0.0
+    ep = edz + rounded * dz.abs()
+    for name, got, a, b, ea_, n in (("dx", grads["dx"], dz, ref["W"].t(), ep @ ref["W"].abs().t(), dz.shape[1]),
+                                    ("dW", grads["dW"], ref["x"].t(), dz, ref["x"].abs().t() @ ep, M)):
+        want = a @ b
+        e = ea_ + (n + 2) * U32 * (a.abs() @ b.abs())
+        close(name, got, want, u * (want.abs() + e) + e, (math.sqrt(n) + 16) * U32 + u + rounded)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_parts_that_may_be_left_out(dtype):
+    """z not asked for, gradients one at a time, db alone without z, residual in place: the same bits."""
+    M, K, N = 70, 136, 264
+    _, dev = linear_case(M, K, N, "relu", dtype, 5)
+    op = SwitchLinear(M, K, N, "relu", 0.25, 9, dtype, DEV, train=True)
+    y = op.forward(dev["x"], dev["W"], dev["bias"], dev["residual"]).clone()
+    g = {k: v.clone() for k, v in op.backward(dev["dy"], dev["x"], dev["W"]).items()}
+    inplace = dev["residual"].clone()
+    sw.switch_linear(op.cfg, dev["x"], dev["W"], dev["bias"], inplace, inplace, None, op.workspace, op.workspace_bytes)
+    assert torch.equal(inplace, y)
+    for name in ("dx", "dW", "db"):
+        out = torch.full_like(g[name], float("nan"))
+        sw.switch_linear_backward(op.cfg, dev["dy"], dev["x"] if name == "dW" else None, dev["W"] if name == "dx" else None,
+                                  op.z, *[out if n == name else None for n in ("dx", "dW", "db")], op.workspace,
+                                  op.workspace_bytes)
+        assert torch.equal(out, g[name]), name
+    plain = SwitchLinear(M, K, N, "none", 0.0, 0, dtype, DEV, train=True)
+    db = plain.backward(dev["dy"], dev["x"], dev["W"])["db"].clone()
+    assert torch.allclose(db.cpu().double(), dev["dy"].cpu().double().sum(0), rtol=0, atol=M * M * U32 * 4)
+    with pytest.raises(ValueError):
+        SwitchLinear(M, K, N, dtype=dtype).backward(dev["dy"], dev["x"], dev["W"])
+    with pytest.raises(ValueError):
+        op.forward(dev["x"][:, ::2], dev["W"])
+    with pytest.raises(ValueError):
+        op.forward(dev["x"].double(), dev["W"])
+
+
+def test_linear_without_rows():
+    op = SwitchLinear(0, 64, 128, "gelu", 0.1, 3, "bf16", DEV, train=True)
+    for t in (op.dW, op.db):
+        t.fill_(7.0)
+    op.forward(torch.empty(0, 64, dtype=torch.bfloat16, device=DEV), torch.ones(64, 128, dtype=torch.bfloat16, device=DEV))
+    g = op.backward(torch.empty(0, 128, dtype=torch.bfloat16, device=DEV), torch.empty(0, 64, dtype=torch.bfloat16, device=DEV),
+                    torch.ones(64, 128, dtype=torch.bfloat16, device=DEV))
+    assert not g["dW"].any() and not g["db"].any()
+
+
+def test_rows_beyond_the_last_stay_as_they_were():
+    """Outputs of M rows in the middle of a larger buffer: nothing before or behind them is written."""
+    for M in (1, 17, 100, 300):
+        for dtype in ("bf16", "f32"):
+            _, dev = linear_case(M, 72, 136, "geglu", dtype, M)
+            op = SwitchLinear(M, 72, 136, "geglu", 0.0, 0, dtype, DEV, train=True)
+            shapes = {"y": (M, 136), "z": (M, 272), "dx": (M, 72), "dW": (72, 272)}
+            big = {k: torch.full((s[0] + 64, s[1]), 3.0, dtype=DT[dtype], device=DEV) for k, s in shapes.items()}
+            for k, s in shapes.items():
+                setattr(op, k, big[k][32:32 + s[0]])
+            op.forward(dev["x"], dev["W"])
+            op.backward(dev["dy"], dev["x"], dev["W"])
+            for k, s in shapes.items():
+                assert (big[k][:32] == 3.0).all() and (big[k][32 + s[0]:] == 3.0).all(), (k, M, dtype)
+                assert not (big[k][32:32 + s[0]] == 3.0).all(), (k, M, dtype)
+
+
+@pytest.mark.parametrize("act", ["gelu", "geglu"])
+def test_linear_gradients_against_differences(act):
+    """Directional differences of the definition in 64 bits; a second-order difference with step h is off by
+    h^2 / 6 of third derivatives of order one, 1e-9 here, the fp32 gradients by their sums' rounding."""
+    M, K, N = 37, 40, 48
+    ref, dev = linear_case(M, K, N, act, "f32", 3)
+    op = SwitchLinear(M, K, N, act, 0.25, 77, "f32", DEV, train=True)
+    op.forward(dev["x"], dev["W"], dev["bias"], dev["residual"])
+    grads = op.backward(dev["dy"], dev["x"], dev["W"])
+    factor = keep_factor(M * N, 0.25, 77).reshape(M, N)
+    loss = lambda x, W, b: (ref["dy"] * act64(act, x @ W + b) * factor).sum()
+    gen = torch.Generator().manual_seed(8)
+    h = 1e-4
+    for name, at in (("dx", 0), ("dW", 1), ("db", 2)):
+        args = [ref["x"], ref["W"], ref["bias"]]
+        v = normal(gen, *args[at].shape)
+        up, down = list(args), list(args)
+        up[at], down[at] = args[at] + h * v, args[at] - h * v
+        diff = (loss(*up) - loss(*down)) / (2 * h)
+        got = (grads[name].cpu().double() * v).sum()
+        scale = (grads[name].cpu().double() * v).abs().sum()
+        assert abs(got - diff) <= scale * (math.sqrt(2 * max(M, N)) + 16) * U32 + 1e-6 * scale, name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rate", [0.0, 1e-6, 0.1, 0.5, 0.999])
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 255, 2048, 2049, 100003, 1 << 20])
+def test_dropout(n, rate, dtype):
+    gen = torch.Generator().manual_seed(n)
+    x, r = normal(gen, n).to(DT[dtype]), normal(gen, n).to(DT[dtype])
+    seed = 0xFEDCBA9876543210 ^ n
+    factor = keep_factor(n, rate, seed)
+    for res in (None, r):
+        guard = torch.full((n + 64,), 5.0, dtype=DT[dtype], device=DEV)
+        y = guard[:n]
+        dropout(x.to(DEV), rate, seed, None if res is None else res.to(DEV), out=y)
+        want = x.double() * factor + (0.0 if res is None else r.double())
+        # the scale and the product rounded to fp32, the sum to the type
+        bound = U[dtype] * want.abs() + 4 * U32 * ((x.double() * factor).abs() + want.abs())
+        assert ((y.cpu().double() - want).abs() <= bound).all()
+        assert (guard[n:] == 5.0).all()
+    # in place, of x and of the residual
+    a, b = x.to(DEV), r.to(DEV)
+    first = dropout(a, rate, seed, b).clone()
+    c, d = a.clone(), b.clone()
+    assert torch.equal(dropout(c, rate, seed, d, out=c), first)
+    c = a.clone()
+    assert torch.equal(dropout(c, rate, seed, d, out=d), first)
+
+
+def test_dropout_draws_like_the_expert_dropout_of_another_stream():
+    """Each bit kept with its rate, alike for even and odd elements, and other masks for other seeds."""
+    n = 1 << 22
+    x = torch.ones(n, device=DEV)
+    a, b = dropout(x, 0.25, 1), dropout(x, 0.25, 2)
+    for part in (a[::2], a[1::2], b):
+        share = float((part == 0).double().mean())
+        assert abs(share - 0.25) < 6 * math.sqrt(0.25 * 0.75 / part.numel())
+    both = float(((a == 0) & (b == 0)).double().mean())
+    assert abs(both - 0.0625) < 6 * math.sqrt(0.0625 * 0.9375 / n)
+
+
+def test_dropout_past_32_bits():
+    """Byte offsets, elements and draws past 32 bits: 2^33 + 200 elements of bf16, in place."""
+    n = (1 << 33) + 200
+    x = torch.ones(n, dtype=torch.bfloat16, device=DEV)
+    dropout(x, 0.5, 11, out=x)
+    for first in (0, (1 << 31) - 50, (1 << 32) - 50, (1 << 33) - 50, n - 100):
+        want = keep_factor(100, 0.5, 11, first)
+        assert torch.equal(x[first:first + 100].cpu().double(), want), first
+
+
+def balance64(logits, index, mask, groups, alpha, d_loss=1.0):
+    T, E = logits.shape
+    valid = torch.ones(T, dtype=torch.bool) if mask is None else mask != 0
+    h = torch.where(valid[:, None], logits, 0.0)
+    top = h.max(1, keepdim=True).values
+    e = torch.exp(h - torch.where(torch.isinf(top), 0.0, top))
+    total = e.sum(1, keepdim=True)
+    p = torch.where(valid[:, None] & (total > 0), e / total.clamp(min=1e-300), 0.0)
+    Tg = T // groups
+    counts = torch.zeros(groups, E, dtype=torch.int64)
+    for g in range(groups):
+        rows = index[g * Tg:(g + 1) * Tg][valid[g * Tg:(g + 1) * Tg]].reshape(-1).long()
+        rows = rows[(rows >= 0) & (rows < E)]
+        counts[g] = torch.bincount(rows, minlength=E)
+    tokens = valid.reshape(groups, Tg).sum(1)
+    n = tokens.double().clamp(min=1)[:, None]
+    f = counts.double() / (n * index.shape[1])
+    P = p.reshape(groups, Tg, E).sum(1) / n
+    loss = alpha * E / groups * (f * P).sum()
+    c = (d_loss * alpha * E / groups * f / n).repeat_interleave(Tg, dim=0)
+    return loss, counts, tokens, p * (c - (p * c).sum(1, keepdim=True)), p, c
+
+
+BALANCE = [(1, 1, 1, 1), (1, 8, 2, 1), (7, 2, 1, 1), (64, 4, 1, 2), (100, 5, 3, 4), (513, 16, 1, 1), (300, 31, 2, 3),
+           (1000, 33, 1, 1), (2049, 64, 2, 1), (777, 100, 4, 1), (4096, 128, 1, 8), (555, 129, 2, 5), (600, 250, 1, 1),
+           (256, 500, 3, 2), (130, 1000, 2, 1), (96, 1026, 1, 3), (70, 2048, 2, 1), (64, 2050, 8, 2), (33, 4096, 1, 1),
+           (20000, 3, 1, 1)]
+
+
+@pytest.mark.parametrize("kind", ["all", "padded", "none of a group", "cut"])
+@pytest.mark.parametrize("T,E,k,groups", BALANCE)
+def test_balance_loss_and_gradient(T, E, k, groups, kind):
+    gen = torch.Generator().manual_seed(T * 3 + E)
+    logits = (2.0 * normal(gen, T, E) + normal(gen, E)).float()
+    index = torch.topk(logits, k, dim=1).indices.to(torch.int32)
+    mask = None
+    if kind in ("padded", "none of a group"):
+        mask = (torch.rand(T, generator=gen) < 0.7).to(torch.uint8) * 3   # any value but 0 is a token
+        if kind == "none of a group":
+            mask[:T // groups] = 0
+        logits[mask == 0] = float("nan")   # what stands in padding means nothing
+        index[mask == 0] = 1 << 30
+    if kind == "cut":   # experts that a token may not choose, a row of nothing else, choices that do not count
+        logits[torch.rand(T, E, generator=gen) < 0.3] = float("-inf")
+        logits[T // 2] = float("-inf")
+        index[::3, 0] = -1
+        index[1::5, 0] = E
+    loss, counts, tokens, want, p, c = balance64(logits.double(), index, mask, groups, 0.5)
+    op = SwitchBalanceLoss(T, E, k, 0.5, groups, DEV)
+    dev = [t if t is None else t.to(DEV) for t in (logits, index, mask)]
+    for t in (op.loss, op.expert_counts, op.token_counts):
+        t.fill_(99)
+    op.workspace.fill_(255)
+    out = op.forward(dev[0], dev[1], dev[2])
+    first = {k_: v.clone() for k_, v in out.items()}
+    got = op.backward(dev[0], dev[2], 1.0).cpu().double()
+    assert torch.equal(out["expert_counts"].cpu().long(), counts)
+    assert torch.equal(out["token_counts"].cpu().long(), tokens)
+    # a probability is off by the exponential (argument up to 20: 20 2^-24 and 2 steps), the row's sum and the division
+    rel = 40 * U32
+    assert abs(float(out["loss"]) - float(loss)) <= (rel + 16 * U32) * abs(float(loss)) + 1e-30
+    spread = (p * (c - c.mean(1, keepdim=True)).abs()).sum(1, keepdim=True) + (c - c.mean(1, keepdim=True)).abs()
+    assert ((got - want).abs() <= p * spread * (3 * rel) + 1e-37).all()
+    assert (got[~torch.isfinite(logits).any(1)] == 0).all()
+    # the same bits again, and in place
+    again = op.forward(dev[0], dev[1], dev[2])
+    assert all(torch.equal(again[k_], first[k_]) for k_ in first)
+    op.dlogits = dev[0]
+    assert torch.equal(op.backward(dev[0], dev[2], 1.0).cpu().double(), got)
+
+
+def test_balance_gradient_against_differences():
+    """d loss / d logits by differences of the definition with the counts held; h^2 / 6 = 2e-9 of the third derivative."""
+    T, E, k, groups, h = 24, 12, 2, 2, 1e-4
+    gen = torch.Generator().manual_seed(4)
+    logits = normal(gen, T, E).float()
+    index = torch.topk(logits, k, dim=1).indices.to(torch.int32)
+    op = SwitchBalanceLoss(T, E, k, 0.3, groups, DEV)
+    op.forward(logits.to(DEV), index.to(DEV))
+    got = op.backward(logits.to(DEV), d_loss=-2.0).cpu().double()
+    v = normal(gen, T, E)
+    diff = -2.0 * (balance64(logits.double() + h * v, index, None, groups, 0.3)[0]
+                   - balance64(logits.double() - h * v, index, None, groups, 0.3)[0]) / (2 * h)
+    scale = float((got * v).abs().sum())
+    assert abs(float((got * v).sum() - diff)) <= scale * (120 * U32 + 1e-6)
+
+
+def test_balance_without_tokens():
+    op = SwitchBalanceLoss(0, 6, 1, 0.1, 1, DEV)
+    op.loss.fill_(1.0)
+    out = op.forward(torch.empty(0, 6, device=DEV), torch.empty(0, 1, dtype=torch.int32, device=DEV))
+    assert float(out["loss"]) == 0.0 and not out["expert_counts"].any() and not out["token_counts"].any()
+    assert op.backward(torch.empty(0, 6, device=DEV)).shape == (0, 6)
+
+
+# ---- together -------------------------------------------------------------------------------
+class Block:
+    """Dense gated-GELU sublayer with dropout and residual, then a Switch sublayer with dropout and residual, whose
+    router's loss is taken over the tokens that are not padding; forward and backward."""
+
+    def __init__(self, T=515, d=64, f=136, E=6):
+        gen = torch.Generator().manual_seed(1)
+        t = lambda *s, k=1.0: (normal(gen, *s) * k).to(torch.bfloat16).to(DEV)
+        self.x, self.dy = t(T, d), t(T, d)
+        self.W1, self.W2 = t(d, 2 * f, k=d ** -0.5), t(f, d, k=f ** -0.5)
+        self.b1 = normal(gen, 2 * f).float().to(DEV)
+        self.W_r = (normal(gen, d, E) * 0.3).float().to(DEV)
+        self.W_in, self.W_out = t(E, d, f, k=d ** -0.5), t(E, f, d, k=f ** -0.5)
+        self.mask = (torch.arange(T) % 128 < 100).to(torch.uint8).to(DEV)
+        self.up = SwitchLinear(T, d, f, "geglu", 0.1, 21, "bf16", DEV, train=True)
+        self.down = SwitchLinear(T, f, d, "none", 0.1, 22, "bf16", DEV, train=True)
+        self.layer = SwitchLayer(T, d, f, E, 2.0, 0.01, "bf16", DEV, want_logits=True)
+        self.layer.alloc_grads(with_bias=False)
+        self.balance = SwitchBalanceLoss(T, E, 1, 0.01, 1, DEV)
+        self.all = SwitchBalanceLoss(T, E, 1, 0.01, 1, DEV)
+        self.y, self.dh, self.dx = (torch.empty_like(self.x) for _ in range(3))
+
+    def step(self):
+        a = self.up.forward(self.x, self.W1, self.b1)
+        h = self.down.forward(a, self.W2, residual=self.x)
+        out = self.layer.forward(h, self.W_r, self.W_in, self.W_out)
+        dropout(out["y"], 0.1, 23, h, out=self.y)
+        loss = self.balance.forward(out["router_logits"], out["expert_index"], self.mask)
+        every = self.all.forward(out["router_logits"], out["expert_index"])
+        dlogits = self.balance.backward(out["router_logits"], self.mask)
+        dropout(self.dy, 0.1, 23, out=self.dh)
+        g = self.layer.backward(self.dh, h, self.W_r, self.W_in, self.W_out, d_aux=0.0)
+        dropout(g["dx"], 0.0, 0, self.dy, out=self.dh)        # the residual's gradient
+        g2 = self.down.backward(self.dh, a, self.W2, with_bias=False)
+        g1 = self.up.backward(g2["dx"], self.x, self.W1)
+        dropout(g1["dx"], 0.0, 0, self.dh, out=self.dx)
+        return [self.y, loss["loss"], loss["expert_counts"], loss["token_counts"], every["loss"], every["expert_counts"],
+                out["aux_loss"], out["expert_counts"], dlogits, g["dW_in"], g["dW_out"], g2["dW"], g1["dW"], g1["db"], self.dx]
+
+
+def test_block_eager_captured_and_on_another_stream():
+    block = Block()
+    want = [t.clone() for t in block.step()]
+    torch.cuda.synchronize()
+    assert all(torch.isfinite(t.float()).all() for t in want)
+    # the layer's own loss over all tokens, from the operator
+    assert torch.equal(want[5][0], want[7])
+    assert abs(float(want[4]) - float(want[6])) <= 1e-5 * float(want[6])
+    assert int(want[3]) == int(block.mask.sum())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for t in block.step():
+            pass
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(block.step(), want))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = block.step()
+    for _ in range(3):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(outs, want)):
+            assert torch.equal(a, b), i
+        block.step()      # eager work between the replays
+        torch.cuda.synchronize()
