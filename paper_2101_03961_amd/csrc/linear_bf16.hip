@@ -1,0 +1,528 @@
+// switch_linear's products on bf16 MFMA, fp32 accumulation.
+//
+// Two kinds of tile.  Large ones, 256 x 256 in eight waves of 64 x 128 (MFMA 16x16x32; P is the "A" side), by persistent
+// blocks, one per CU: the loads run one (Q) and two (P) steps of 64 k ahead of the products, over the end of a tile into the
+// block's next one, so that a tile's first loads and its stores overlap with products.  Small ones, 128 x 128 in four waves, two
+// blocks per CU, for products with too few large tiles.
+#include <math.h>
+
+#include "linear.h"
+#include "rows_operands.h"
+
+namespace sw {
+
+constexpr int BK = 64;   // k per step
+
+// [k][row] operand of the gated activation: tile columns come in groups of 32 IP per wave, half of them gate
+// columns and half the linear columns that belong to them.
+template <int IP, int WP, int NW> struct GatedTrans : RowsTrans<32 * IP * WP, NW> {
+    typedef RowsTrans<32 * IP * WP, NW> Base;
+    __device__ __forceinline__ void init_gated(const bf16 *base, int ld, int col0, int cols, int klim, int lane, int wave) {
+        constexpr int R = 32 * IP * WP;
+        Base::init(base, ld, 0, ld, klim, lane, wave);
+#pragma unroll
+        for (int i = 0; i < Base::kPeriod; ++i) {
+            const int at = (R == 256 ? 0 : wave * Base::kGroup + i) * 64 + lane;
+            const int kr = at / Base::kChunks + (R == 256 ? Base::first_row(wave, 0) : 0);
+            const int r = (at % Base::kChunks ^ Base::perm(kr)) << 3;
+            const int w = r / (32 * IP), in = r % (32 * IP);
+            const bool linear = in >= 16 * IP;
+            const int col = col0 + w * (16 * IP) + (linear ? in - 16 * IP : in);
+            this->voff[i] = col < cols ? ((uint32_t)kr * (uint32_t)ld + (uint32_t)(linear ? cols + col : col)) * 2u
+                                       : kOobOffset;
+        }
+    }
+};
+
+struct LinearTiles {
+    int tiles_q, tiles_p;
+    int splits;
+    int64_t split_k;
+};
+
+// A tile's place: item n of the product.  Items of a part of k are neighbours, in bands of eight row tiles, so that
+// those that run on an XCD at a time, 32 in a row, share their operands in its L2.
+struct LinearPlace {
+    int64_t q0, k0;
+    int p0, split, klim;
+};
+template <int QB, int OUTP, LinearKind KIND>
+__device__ __forceinline__ LinearPlace linear_place(const LinearArgs &a, const LinearTiles &t, int n) {
+    LinearPlace at;
+    const int tiles = t.tiles_q * t.tiles_p;
+    at.split = KIND == LINEAR_DW ? n / tiles : 0;
+    n -= at.split * tiles;
+    constexpr int kBand = 8;
+    const int band = n / (kBand * t.tiles_p), rows = min(kBand, t.tiles_q - band * kBand);
+    n -= band * kBand * t.tiles_p;
+    const int pt = n / rows;
+    at.q0 = (int64_t)(band * kBand + (n - pt * rows)) * QB;
+    at.p0 = pt * OUTP;
+    at.k0 = at.split * t.split_k;
+    at.klim = (int)(KIND == LINEAR_DW && a.Kdim - at.k0 > t.split_k ? t.split_k : a.Kdim - at.k0);
+    return at;
+}
+
+// The operands' loads of a tile.  (Descriptors span 32 bits: W is below 2 GB; a tile's rows of x and dz, and a part's rows of
+// both, begin at the base.)
+template <LinearKind KIND, bool GATED, typename OP>
+__device__ __forceinline__ void linear_init_p(OP &op, const LinearArgs &a, const LinearPlace &at, int lane, int wave) {
+    if constexpr (GATED) op.init_gated((const bf16 *)a.P, a.ldp, at.p0, a.Pdim, at.klim, lane, wave);
+    else
+        op.init((const bf16 *)a.P + (KIND == LINEAR_DW ? (size_t)at.k0 * a.ldp : 0), a.ldp, at.p0, a.Pdim, at.klim, lane, wave);
+}
+template <LinearKind KIND, int QB, typename OQ>
+__device__ __forceinline__ void linear_init_q(OQ &oq, const LinearArgs &a, const LinearPlace &at, int lane, int wave) {
+    if constexpr (KIND == LINEAR_DW)
+        oq.init((const bf16 *)a.Q + (size_t)at.k0 * a.ldq, a.ldq, (int)at.q0, (int)a.Qdim, at.klim, lane, wave);
+    else
+        oq.init((const bf16 *)a.Q + (size_t)at.q0 * a.ldq, a.ldq, 0, (int)min(a.Qdim - at.q0, (int64_t)QB), at.klim, lane, wave);
+}
+
+// Epilogue of a wave: 16 rows at a time through 2 KB IP of LDS of its own, as fp32, so that a lane has eight consecutive
+// columns (of the gate and the linear part) and rows leave in whole segments.  The 16-byte chunks of a row trade places by
+// the row, so that neither side has bank conflicts.
+template <int IP, int IQ, int WQ, LinearKind KIND, int ACT>
+__device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const LinearTiles &t, const LinearPlace &at,
+                                                const f32x4 (&acc)[2 * IP][2 * IQ], char *turn, int lane, int wp, int wq) {
+    static_assert(IP % 2 == 0, "whole groups of 16 chunks of a row");
+    constexpr bool GATED = ACT == SW_ACT_GEGLU;
+    constexpr int kPitch = 32 * IP * 4, kCols = GATED ? 16 * IP : 32 * IP, kChunks = kCols / 8;
+    constexpr int kPasses = 16 * kChunks / 64, kPassRows = 64 / kChunks;
+    const int r0 = lane / kChunks, c = lane % kChunks;   // the lane's row, those kPassRows further, and its chunk
+    const int p = at.p0 + wp * kCols + c * 8;
+    if (at.p0 + wp * kCols >= a.Pdim) return;
+    const int rows = (int)min(a.Qdim - at.q0, (int64_t)0x7fffffff) - wq * IQ * 32;   // of the wave
+    const int64_t q0 = at.q0 + wq * IQ * 32;
+    const bool in = p < a.Pdim;
+    float bu[8], bv[8];
+    if (KIND == LINEAR_FWD && a.bias && in) {
+        Eight<float>::load(a.bias + p, bu);
+        if (GATED) Eight<float>::load(a.bias + a.Pdim + p, bv);
+    }
+    const int64_t Nz = GATED ? 2 * (int64_t)a.Pdim : a.Pdim;
+#pragma unroll
+    for (int j = 0; j < 2 * IQ; ++j) {
+        if (j * 16 >= rows) break;
+        bf16x8 res[kPasses];
+        if (KIND == LINEAR_FWD && a.residual) {
+#pragma unroll
+            for (int x = 0; x < kPasses; ++x) {
+                const int row = j * 16 + x * kPassRows + r0;
+                if (row < rows && in) res[x] = *(const bf16x8 *)((const bf16 *)a.residual + (q0 + row) * a.Pdim + p);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * IP; ++i)
+            *(f32x4 *)(turn + (lane & 15) * kPitch + (((i * 4 + (lane >> 4)) ^ (lane & 15)) << 4)) = acc[i][j];
+#pragma unroll
+        for (int x = 0; x < kPasses; ++x) {
+            const int r = x * kPassRows + r0, row = j * 16 + r;
+            auto chunk = [&](int n) { return *(const f32x4 *)(turn + r * kPitch + ((n ^ r) << 4)); };
+            float v[8], lin[8];
+            *(f32x4 *)v = chunk(2 * c);
+            *(f32x4 *)(v + 4) = chunk(2 * c + 1);
+            if (GATED) {
+                *(f32x4 *)lin = chunk(2 * c + kCols / 4);
+                *(f32x4 *)(lin + 4) = chunk(2 * c + 1 + kCols / 4);
+            }
+            if (row >= rows || !in) continue;
+            const int64_t q = q0 + row, out = q * a.Pdim + p;
+            if (KIND == LINEAR_DW && t.splits > 1) {
+                Eight<float>::store(a.part + ((int64_t)at.split * a.Qdim * a.Pdim + out), v);
+                continue;
+            }
+            if (KIND != LINEAR_FWD) {
+#pragma unroll
+                for (int m = 0; m < 8; ++m) v[m] *= a.scale;
+            } else {
+                if (a.bias) {
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) {
+                        v[m] += bu[m];
+                        if (GATED) lin[m] += bv[m];
+                    }
+                }
+                if (a.z) {
+                    Eight<bf16>::store((bf16 *)a.z + q * Nz + p, v);
+                    if (GATED) Eight<bf16>::store((bf16 *)a.z + q * Nz + a.Pdim + p, lin);
+                }
+#pragma unroll
+                for (int m = 0; m < 8; ++m) v[m] = linear_act(ACT, v[m], GATED ? lin[m] : 0.f);
+                if (a.drop.on) {
+                    drop_apply<8>(a.drop, (uint64_t)out, v);
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) v[m] *= a.drop.scale;
+                }
+                if (a.residual)
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) v[m] += (float)res[x][m];
+            }
+            Eight<bf16>::store((bf16 *)a.C + out, v);
+        }
+    }
+}
+
+template <int IP, int WP, int IQ, int WQ, LinearKind KIND, bool GATED> struct LinearOps {
+    static constexpr int NW = WP * WQ, PB = 32 * IP * WP, QB = 32 * IQ * WQ, OUTP = GATED ? PB / 2 : PB;
+    typedef typename std::conditional<KIND == LINEAR_DX, RowsDirect<PB, NW>,
+        typename std::conditional<GATED, GatedTrans<IP, WP, NW>, RowsTrans<PB, NW>>::type>::type P;
+    typedef typename std::conditional<KIND == LINEAR_DW, RowsTrans<QB, NW>, RowsDirect<QB, NW>>::type Q;
+    static constexpr int kPBytes = PB * BK * 2, kStage = (PB + QB) * BK * 2;
+    static constexpr int kTurn = 16 * 32 * IP * 4;   // bytes per wave
+};
+
+// Four products into four accumulators, which stay where they are: the compiler's own copies some of 64 around between the
+// registers of either kind.  With a direct load (see dma16) behind them, whose m0 is set before them: the products are the
+// wait states between that, or a descriptor reloaded from a spill lane, and the load.
+__device__ __forceinline__ void products4(f32x4 &c0, f32x4 &c1, f32x4 &c2, f32x4 &c3, bf16x8 p0, bf16x8 p1, bf16x8 p2, bf16x8 p3,
+                                          bf16x8 q) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %4, %8, %0\n\t"
+                 "v_mfma_f32_16x16x32_bf16 %1, %5, %8, %1\n\t"
+                 "v_mfma_f32_16x16x32_bf16 %2, %6, %8, %2\n\t"
+                 "v_mfma_f32_16x16x32_bf16 %3, %7, %8, %3"
+                 : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3)
+                 : "v"(p0), "v"(p1), "v"(p2), "v"(p3), "v"(q));
+}
+__device__ __forceinline__ void products4_load(f32x4 &c0, f32x4 &c1, f32x4 &c2, f32x4 &c3, bf16x8 p0, bf16x8 p1, bf16x8 p2,
+                                               bf16x8 p3, bf16x8 q, i32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %12\n\t"
+                 "v_mfma_f32_16x16x32_bf16 %0, %4, %8, %0\n\t"
+                 "v_mfma_f32_16x16x32_bf16 %1, %5, %8, %1\n\t"
+                 "v_mfma_f32_16x16x32_bf16 %2, %6, %8, %2\n\t"
+                 "v_mfma_f32_16x16x32_bf16 %3, %7, %8, %3\n\t"
+                 "buffer_load_dwordx4 %9, %10, %11 offen lds"
+                 : "+a"(c0), "+a"(c1), "+a"(c2), "+a"(c3)
+                 : "v"(p0), "v"(p1), "v"(p2), "v"(p3), "v"(q), "v"(voff), "s"(rsrc), "s"(soff), "s"(lds)
+                 : "memory");
+}
+
+// One large tile: four waves of 128 x 128, one per SIMD, whose fragments take a third less LDS traffic than those of eight
+// waves of 64 x 128 (1536 cycles of reads and fills per step, the products take 2048).  P goes through three stages of 32 KB, Q
+// through two: at the middle of step kt, when both stages of kt are read, the loads of Q for step kt + 2 and of P for kt + 3
+// begin to fill them.  The fragments of a half step are read during the products of the half step before.
+template <LinearKind KIND, int ACT>
+__device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTiles &t, char *lds, int n) {
+    constexpr int IP = 4, WP = 2, IQ = 4, WQ = 2;
+    constexpr bool GATED = ACT == SW_ACT_GEGLU;
+    typedef LinearOps<IP, WP, IQ, WQ, KIND, GATED> S;
+    constexpr int kStageP = S::PB * BK * 2, kStageQ = S::QB * BK * 2;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wp = wave % WP, wq = wave / WP;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const LinearPlace at = linear_place<S::QB, S::OUTP, KIND>(a, t, n);
+    typename S::P op;
+    typename S::Q oq;
+    constexpr int kLoadsP = S::P::kLoads, kLoadsQ = S::Q::kLoads;
+    static_assert(kLoadsP + kLoadsQ == 16, "a load per group of products");
+    op.init_frag16(lane, wp * 32 * IP);
+    oq.init_frag16(lane, wq * 32 * IQ);
+    linear_init_p<KIND, GATED>(op, a, at, lane, wave);
+    linear_init_q<KIND, S::QB>(oq, a, at, lane, wave);
+    f32x4 acc[2 * IP][2 * IQ];
+#pragma unroll
+    for (int i = 0; i < 2 * IP; ++i)
+#pragma unroll
+        for (int j = 0; j < 2 * IQ; ++j) {
+            acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            asm volatile("" : "+a"(acc[i][j]));
+        }
+    asm volatile("s_nop 3");   // written before the first product reads them
+    const int nk = (at.klim + BK - 1) / BK;
+    auto issue_p = [&](uint32_t st, int kt, int i) { op.issue_one(lds0 + st, kt * BK, wave, i); };
+    auto issue_q = [&](uint32_t st, int kt, int i) { oq.issue_one(lds0 + 3 * kStageP + st, kt * BK, wave, i); };
+#pragma unroll
+    for (int s = 0; s < 3; ++s) {
+#pragma unroll
+        for (int i = 0; i < kLoadsP; ++i) issue_p(s * kStageP, s, i);
+#pragma unroll
+        for (int i = 0; i < kLoadsQ; ++i)
+            if (s < 2) issue_q(s * kStageQ, s, i);
+    }
+    rows_wait_vmcnt<2 * kLoadsP + kLoadsQ>();
+    __syncthreads();
+    bf16x8 fp[2][2 * IP], fq[2][2 * IQ];
+    // fragment f of a half step, in the order of use
+    auto read = [&](const char *sp, const char *sq, int ks, int f) {
+        if (f == 0) fq[ks][0] = oq.frag16(sq, 0, ks);
+        else if (f <= 2 * IP) fp[ks][f - 1] = op.frag16(sp, f - 1, ks);
+        else fq[ks][f - 2 * IP] = oq.frag16(sq, f - 2 * IP, ks);
+    };
+    constexpr int kGroups = 2 * IP + 2 * IQ;   // fragments, and groups of four products, of a half step
+    static_assert(kGroups == 16 && 4 * IP * IQ == 4 * kGroups, "four products per fragment");
+#pragma unroll
+    for (int f = 0; f < kGroups; ++f) read(lds, lds + 3 * kStageP, 0, f);
+    uint32_t sp = 0, sq = 0;   // stages of step kt
+#pragma nounroll
+    for (int kt = 0; kt < nk; ++kt) {
+        const uint32_t sp1 = sp == 2 * kStageP ? 0 : sp + kStageP, sq1 = sq ^ kStageQ;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            op.reload_frag();
+            oq.reload_frag();
+            if (ks == 1) {
+                rows_wait_vmcnt<kLoadsP>();   // step kt + 1 has landed
+                asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+                __syncthreads();              // ... for all waves, and both stages of step kt are read
+            }
+            const char *rp = lds + (ks == 0 ? sp : sp1), *rq = lds + 3 * kStageP + (ks == 0 ? sq : sq1);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                // (the last four groups of the first half cover the reads' latency before the barrier)
+                if (ks == 1 || g < 8) read(rp, rq, ks ^ 1, g);
+                if (ks == 0 && g < 8) read(rp, rq, 1, g + 8);
+                __builtin_amdgcn_sched_barrier(0);
+                const int i = g % 2 * 4, j = g / 2;
+                if (ks == 0) {
+                    products4(acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j], fp[0][i], fp[0][i + 1], fp[0][i + 2],
+                              fp[0][i + 3], fq[0][j]);
+                } else {
+                    i32x4 rsrc;
+                    uint32_t voff, soff, at_lds;
+                    if (g < kLoadsQ) {
+                        oq.load_of((kt + 2) * BK, wave, g, rsrc, voff, soff, at_lds);
+                        at_lds += lds0 + 3 * kStageP + sq;
+                    } else {
+                        op.load_of((kt + 3) * BK, wave, g - kLoadsQ, rsrc, voff, soff, at_lds);
+                        at_lds += lds0 + sp;
+                    }
+                    products4_load(acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j], fp[1][i], fp[1][i + 1], fp[1][i + 2],
+                                   fp[1][i + 3], fq[1][j], rsrc, voff, soff, at_lds);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        sp = sp1;
+        sq = sq1;
+    }
+    rows_wait_vmcnt<0>();   // the trailing loads
+    asm volatile("s_nop 15\n\ts_nop 15");   // the last products (the compiler does not know them as such)
+#pragma unroll
+    for (int i = 0; i < 2 * IP; ++i)
+#pragma unroll
+        for (int j = 0; j < 2 * IQ; ++j) asm volatile("" : "+a"(acc[i][j]));
+    __syncthreads();
+    linear_epilogue<IP, IQ, WQ, KIND, ACT>(a, t, at, acc, lds + wave * S::kTurn, lane, wp, wq);
+}
+
+// item of a block when the blocks of an XCD (b mod 8) take neighbouring ones
+__device__ __forceinline__ int linear_item(int b, int total) {
+    return (b & 7) * ((total + 7) >> 3) + (b >> 3);
+}
+
+template <int ACT>
+__global__ __launch_bounds__(256, 1) void linear_fwd_large_kernel(LinearArgs a, LinearTiles t) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int total = t.tiles_q * t.tiles_p, n = linear_item(blockIdx.x, total);
+    if (n < total) linear_large<LINEAR_FWD, ACT>(a, t, lds, n);
+}
+
+__global__ __launch_bounds__(256, 1) void linear_bwd_large_kernel(LinearArgs dx, LinearTiles tx, LinearArgs dW, LinearTiles tw,
+                                                                  int dx_blocks) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    if ((int)blockIdx.x < dx_blocks) {
+        const int total = tx.tiles_q * tx.tiles_p, n = linear_item(blockIdx.x, total);
+        if (n < total) linear_large<LINEAR_DX, SW_ACT_NONE>(dx, tx, lds, n);
+    } else {
+        const int total = tw.tiles_q * tw.tiles_p * tw.splits, n = linear_item(blockIdx.x - dx_blocks, total);
+        if (n < total) linear_large<LINEAR_DW, SW_ACT_NONE>(dW, tw, lds, n);
+    }
+}
+
+// One small tile: four waves of 64 x 64, two stages.
+template <LinearKind KIND, int ACT>
+__device__ __forceinline__ void linear_small(const LinearArgs &a, const LinearTiles &t, char *lds, int n) {
+    constexpr int IP = 2, WP = 2, IQ = 2, WQ = 2;
+    constexpr bool GATED = ACT == SW_ACT_GEGLU;
+    typedef LinearOps<IP, WP, IQ, WQ, KIND, GATED> S;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wp = wave % WP, wq = wave / WP;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const LinearPlace at = linear_place<S::QB, S::OUTP, KIND>(a, t, n);
+    typename S::P op;
+    typename S::Q oq;
+    op.init_frag16(lane, wp * 32 * IP);
+    oq.init_frag16(lane, wq * 32 * IQ);
+    linear_init_p<KIND, GATED>(op, a, at, lane, wave);
+    linear_init_q<KIND, S::QB>(oq, a, at, lane, wave);
+    f32x4 acc[2 * IP][2 * IQ];
+#pragma unroll
+    for (int i = 0; i < 2 * IP; ++i)
+#pragma unroll
+        for (int j = 0; j < 2 * IQ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto issue = [&](int kt) {
+        const uint32_t to = lds0 + (uint32_t)((kt & 1) * S::kStage);
+#pragma unroll
+        for (int i = 0; i < S::P::kLoads; ++i) op.issue_one(to, kt * BK, wave, i);
+#pragma unroll
+        for (int i = 0; i < S::Q::kLoads; ++i) oq.issue_one(to + S::kPBytes, kt * BK, wave, i);
+    };
+    const int nk = (at.klim + BK - 1) / BK;
+    issue(0);
+    for (int kt = 0; kt < nk; ++kt) {
+        rows_wait_vmcnt<0>();   // step kt has landed
+        __syncthreads();        // ... for all waves; step kt - 1 is read
+        if (kt + 1 < nk) issue(kt + 1);
+        const char *sp = lds + (kt & 1) * S::kStage, *sq = sp + S::kPBytes;
+#pragma unroll
+        for (int ks = 0; ks < BK / 32; ++ks) {
+            bf16x8 fp[2 * IP], fq[2 * IQ];
+#pragma unroll
+            for (int i = 0; i < 2 * IP; ++i) fp[i] = op.frag16(sp, i, ks);
+#pragma unroll
+            for (int j = 0; j < 2 * IQ; ++j) fq[j] = oq.frag16(sq, j, ks);
+#pragma unroll
+            for (int j = 0; j < 2 * IQ; ++j)
+#pragma unroll
+                for (int i = 0; i < 2 * IP; ++i)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i], fq[j], acc[i][j], 0, 0, 0);
+        }
+    }
+    __syncthreads();
+    linear_epilogue<IP, IQ, WQ, KIND, ACT>(a, t, at, acc, lds + wave * S::kTurn, lane, wp, wq);
+}
+
+template <int ACT>
+__global__ __launch_bounds__(256, 2) void linear_fwd_small_kernel(LinearArgs a, LinearTiles t) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int total = t.tiles_q * t.tiles_p, n = linear_item(blockIdx.x, total);
+    if (n < total) linear_small<LINEAR_FWD, ACT>(a, t, lds, n);
+}
+
+__global__ __launch_bounds__(256, 2) void linear_bwd_small_kernel(LinearArgs dx, LinearTiles tx, LinearArgs dW, LinearTiles tw,
+                                                                  int dx_blocks) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    if ((int)blockIdx.x < dx_blocks) {
+        const int total = tx.tiles_q * tx.tiles_p, n = linear_item(blockIdx.x, total);
+        if (n < total) linear_small<LINEAR_DX, SW_ACT_NONE>(dx, tx, lds, n);
+    } else {
+        const int total = tw.tiles_q * tw.tiles_p * tw.splits, n = linear_item(blockIdx.x - dx_blocks, total);
+        if (n < total) linear_small<LINEAR_DW, SW_ACT_NONE>(dW, tw, lds, n);
+    }
+}
+
+// ---- host side ------------------------------------------------------------------------------
+constexpr int kLargeTile = 256, kSmallTile = 128;
+constexpr int kLargeLds = 5 * kLargeTile * BK * 2, kSmallLds = 2 * 2 * kSmallTile * BK * 2;
+static_assert(kLargeLds == 160 * 1024, "all of a CU's");
+constexpr int kCUs = 256;
+
+// us of a step of 64 k and of a tile's start and end, all CUs busy: large tiles one at a time per CU, small ones two
+constexpr double kLargeStep = 1.6, kLargeOnce = 6., kSmallStep = 1.03, kSmallOnce = 6.;
+
+static double rounds_us(double tiles, double slots, double us) { return ceil(tiles / slots) * us; }
+
+LinearPlan plan_linear_bf16(const switch_linear_config *cfg, bool backward) {
+    const int64_t M = cfg->M, K = cfg->K, Nz = linear_columns(cfg);
+    LinearPlan plan{0, 1, M};
+    if (M == 0) return plan;
+    if (!backward) {
+        const double steps = (double)ceil_div(K, BK);
+        const double large = rounds_us((double)(ceil_div(M, 256) * ceil_div(Nz, 256)), kCUs, steps * kLargeStep + kLargeOnce);
+        const double small = rounds_us((double)(ceil_div(M, 128) * ceil_div(Nz, 128)), 2 * kCUs, steps * kSmallStep + kSmallOnce);
+        plan.tile = large <= small ? kLargeTile : kSmallTile;
+        return plan;
+    }
+    // parts of k: at least what the descriptors ask for; more where the tiles leave CUs idle.  A part costs its sums'
+    // store and load.
+    const int64_t widest = K > Nz ? K : Nz, most_k = ((int64_t)0x7fffffff / (2 * widest)) / BK * BK;
+    double best = 1e30;
+    for (int tile : {kLargeTile, kSmallTile}) {
+        const double step = tile == kLargeTile ? kLargeStep : kSmallStep, once = tile == kLargeTile ? kLargeOnce : kSmallOnce;
+        const double slots = tile == kLargeTile ? kCUs : 2 * kCUs;
+        const double tx = (double)(ceil_div(M, tile) * ceil_div(K, tile)), tw = (double)(ceil_div(K, tile) * ceil_div(Nz, tile));
+        const double dx_us = ceil_div(Nz, BK) * step + once;
+        int64_t last = 0;
+        for (int s = 1; s <= 64; ++s) {
+            const int64_t split_k = ceil_div(ceil_div(M, s), BK) * BK, splits = ceil_div(M, split_k);
+            if (split_k > most_k || splits == last) continue;
+            last = splits;
+            const double dw_us = split_k / BK * step + once;
+            // list scheduling: dx's tiles first
+            const double full = floor(tx / slots), over = tx - full * slots, t0 = full * dx_us;
+            const double items = tw * (double)splits;
+            // smallest end at which the blocks have room for the items
+            double end = t0 + (over > 0 ? dx_us : 0.);
+            for (int i = 0; i < 4096; ++i) {
+                const double room = over * floor(fmax(end - t0 - dx_us, 0.) / dw_us + 1e-9) + (slots - over) * floor((end - t0) / dw_us + 1e-9);
+                if (room >= items) break;
+                const double a = t0 + dx_us + (floor(fmax(end - t0 - dx_us, 0.) / dw_us + 1e-9) + 1.) * dw_us;
+                const double b = t0 + (floor((end - t0) / dw_us + 1e-9) + 1.) * dw_us;
+                end = over > 0 && a < b ? a : b;
+            }
+            const double join = splits > 1 ? 4. + (double)splits * K * Nz * 8. / 4e6 : 0.;
+            if (end + join < best) {
+                best = end + join;
+                plan.tile = tile;
+                plan.splits = (int)splits;
+                plan.split_k = split_k;
+            }
+        }
+        if (best > 1e29) {   // (more rows than 64 parts of the widest descriptor hold)
+            plan.tile = tile;
+            plan.split_k = most_k;
+            plan.splits = (int)ceil_div(M, most_k);
+        }
+    }
+    return plan;
+}
+
+static LinearTiles linear_tiles(const LinearArgs &a, int tile, const LinearPlan &plan, bool dW) {
+    LinearTiles t;
+    t.tiles_q = (int)ceil_div(a.Qdim, tile);
+    t.tiles_p = (int)ceil_div(a.Pdim, a.gated ? tile / 2 : tile);
+    t.splits = dW ? plan.splits : 1;
+    t.split_k = dW ? plan.split_k : a.Kdim;
+    return t;
+}
+
+template <typename F> static hipError_t with_lds(PerDeviceOnce &once, F kernel, int bytes) {
+    return once_per_device(once, [&] {
+        return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    });
+}
+
+template <int ACT> static hipError_t linear_fwd_bf16(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
+    const bool large = plan.tile == kLargeTile;
+    const LinearTiles t = linear_tiles(a, plan.tile, plan, false);
+    const int64_t blocks = ceil_div((int64_t)t.tiles_q * t.tiles_p, 8) * 8;
+    auto kern = large ? linear_fwd_large_kernel<ACT> : linear_fwd_small_kernel<ACT>;
+    static PerDeviceOnce once[2];
+    const int lds = large ? kLargeLds : kSmallLds;
+    const hipError_t err = with_lds(once[large], kern, lds);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), lds, s, a, t);
+    return hipGetLastError();
+}
+
+hipError_t launch_linear_bf16(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
+    ProfScope ps("linear", s);
+    switch (a.act) {
+    case SW_ACT_RELU: return linear_fwd_bf16<SW_ACT_RELU>(plan, a, s);
+    case SW_ACT_GELU: return linear_fwd_bf16<SW_ACT_GELU>(plan, a, s);
+    case SW_ACT_GEGLU: return linear_fwd_bf16<SW_ACT_GEGLU>(plan, a, s);
+    default: return linear_fwd_bf16<SW_ACT_NONE>(plan, a, s);
+    }
+}
+
+hipError_t launch_linear_backward_bf16(const LinearPlan &plan, const LinearArgs *dx, const LinearArgs *dW, hipStream_t s) {
+    ProfScope ps("linear_backward", s);
+    const bool large = plan.tile == kLargeTile;
+    const LinearArgs none{};
+    const LinearArgs &ax = dx ? *dx : none, &aw = dW ? *dW : none;
+    const LinearTiles tx = dx ? linear_tiles(ax, plan.tile, plan, false) : LinearTiles{};
+    const LinearTiles tw = dW ? linear_tiles(aw, plan.tile, plan, true) : LinearTiles{};
+    const int64_t bx = ceil_div((int64_t)tx.tiles_q * tx.tiles_p, 8) * 8;
+    const int64_t bw = ceil_div((int64_t)tw.tiles_q * tw.tiles_p * tw.splits, 8) * 8;
+    auto kern = large ? linear_bwd_large_kernel : linear_bwd_small_kernel;
+    static PerDeviceOnce once[2];
+    const int lds = large ? kLargeLds : kSmallLds;
+    const hipError_t err = with_lds(once[large], kern, lds);
+    if (err != hipSuccess) return err;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(bx + bw)), dim3(256), lds, s, ax, tx, aw, tw, (int)bx);
+    return hipGetLastError();
+}
+
+}  // namespace sw

@@ -39,6 +39,14 @@ template <int R, int NW, int BK = 64, bool ONCE = false> struct RowsDirect {
         dma16<ONCE>(rsrc, vo, (uint32_t)i * row_step + (uint32_t)k0 * 2u,
               st + (uint32_t)((i * NW + wave) * 1024));
     }
+    // the same load's operands, for one issued elsewhere (its LDS address from the stage on)
+    __device__ __forceinline__ void load_of(int k0, int wave, int i, i32x4 &desc, uint32_t &vo, uint32_t &so,
+                                            uint32_t &at) const {
+        desc = rsrc;
+        vo = voff | ((uint32_t)(klim - k0 - 1 - c8) & kOobOffset);
+        so = (uint32_t)i * row_step + (uint32_t)k0 * 2u;
+        at = (uint32_t)((i * NW + wave) * 1024);
+    }
     __device__ __forceinline__ bf16x8 frag(const char *st, int x, int ks) const {
         return *(const bf16x8 *)(st + ((frag0 ^ (uint32_t)(ks << 5)) + (uint32_t)(x * 32 * kPitch)));
     }
@@ -145,6 +153,15 @@ template <int R, int NW, int BK = 64, bool ONCE = false> struct RowsTrans {
         const int in = i % kGroup, at = i / kGroup * kRun * NW;
         dma16<ONCE>(rsrc, voff[in % kPeriod], (uint32_t)(k0 + at + in / kPeriod * kPeriodRows) * k_step,
               st + (uint32_t)(at * (R * 2) + (wave * kGroup + in) * 1024));
+    }
+    // (R = 256) the same load's operands, for one issued elsewhere (its LDS address from the stage on)
+    __device__ __forceinline__ void load_of(int k0, int wave, int i, i32x4 &desc, uint32_t &vo, uint32_t &so,
+                                            uint32_t &at) const {
+        static_assert(R == 256, "");
+        desc = rsrc;
+        vo = voff[0];
+        so = (uint32_t)(k0 + first_row(wave, i) - first_row(wave, 0)) * k_step;
+        at = (uint32_t)(first_row(wave, i) * (R * 2));
     }
     __device__ __forceinline__ bf16x8 frag16(const char *st, int x, int ks) const {
         typedef __attribute__((address_space(3))) s16x4 *lds_s16x4_ptr;
