@@ -2,103 +2,13 @@
 //
 //   z = x W + b,  y = r + drop(act(z));   dz = act'(z) drop(dy),  dx = dz W^T,  dW = x^T dz,  db = sum of dz's rows
 //
-// All three products are C[q][p] = sum_k Q(q, k) P(p, k) with C row-major.
+// The products: linear_bf16.hip, linear_f32.hip, linear_few.hip.  Here: how they are cut, the element-wise pass before those of
+// the backward pass, the sums of their parts, and the entry points.
 #include <math.h>
 
 #include "linear.h"
 
 namespace sw {
-
-constexpr int kLinTile = 64, kLinKC = 16;
-
-template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void linear_kernel(LinearArgs a, int kind) {
-    const long q_rs = kind == LINEAR_DW ? 1 : a.ldq, q_ks = kind == LINEAR_DW ? a.ldq : 1;
-    const long p_rs = kind == LINEAR_DX ? a.ldp : 1, p_ks = kind == LINEAR_DX ? 1 : a.ldp;
-    constexpr int NP = GATED ? 2 : 1;
-    __shared__ float qs[kLinKC][kLinTile + 4];
-    __shared__ float ps[NP][kLinKC][kLinTile + 4];
-    const int64_t q0 = (int64_t)blockIdx.x * kLinTile;
-    const int p0 = blockIdx.y * kLinTile;
-    const T *Q = (const T *)a.Q, *P = (const T *)a.P;
-    const int tid = threadIdx.x, tx = tid % 16, ty = tid / 16;
-    float acc[NP][4][4], total[NP][4][4];
-#pragma unroll
-    for (int g = 0; g < NP; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[g][i][j] = total[g][i][j] = 0.f;
-    for (int64_t k0 = 0; k0 < a.Kdim; k0 += kLinKC) {
-        if (k0 % 256 == 0) {
-#pragma unroll
-            for (int g = 0; g < NP; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        total[g][i][j] += acc[g][i][j];
-                        acc[g][i][j] = 0.f;
-                    }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int id = tid + i * 256;
-            int r, kk;
-            if (q_ks == 1) { kk = id % kLinKC; r = id / kLinKC; } else { r = id % kLinTile; kk = id / kLinTile; }
-            qs[kk][r] = q0 + r < a.Qdim && k0 + kk < a.Kdim ? to_f32(Q[(q0 + r) * q_rs + (k0 + kk) * q_ks]) : 0.f;
-            if (p_ks == 1) { kk = id % kLinKC; r = id / kLinKC; } else { r = id % kLinTile; kk = id / kLinTile; }
-#pragma unroll
-            for (int g = 0; g < NP; ++g)
-                ps[g][kk][r] = p0 + r < a.Pdim && k0 + kk < a.Kdim
-                                   ? to_f32(P[(long)(g * a.Pdim + p0 + r) * p_rs + (k0 + kk) * p_ks]) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < kLinKC; ++kk)
-#pragma unroll
-            for (int g = 0; g < NP; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        acc[g][i][j] = fmaf(qs[kk][ty * 4 + i], ps[g][kk][tx * 4 + j], acc[g][i][j]);
-        __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t q = q0 + ty * 4 + i;
-        if (q >= a.Qdim) continue;
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-            const int p = p0 + tx * 4 + j;   // Pdim is even
-            if (p >= a.Pdim) continue;
-            float v[2];
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                float z[NP];
-#pragma unroll
-                for (int g = 0; g < NP; ++g) {
-                    z[g] = (total[g][i][j + m] + acc[g][i][j + m]) * a.scale;
-                    if (a.bias) z[g] += a.bias[g * a.Pdim + p + m];
-                    if (a.z) ((T *)a.z)[q * a.Pdim * NP + g * a.Pdim + p + m] = from_f32<T>(z[g]);
-                }
-                v[m] = linear_act(a.act, z[0], z[NP - 1]);
-            }
-            const int64_t at = q * a.Pdim + p;
-            if (a.drop.on) {
-                drop_apply<2>(a.drop, (uint64_t)at, v);
-                v[0] *= a.drop.scale;
-                v[1] *= a.drop.scale;
-            }
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                if (a.residual) v[m] += to_f32(((const T *)a.residual)[at + m]);
-                ((T *)a.C)[at + m] = from_f32<T>(v[m]);
-            }
-        }
-    }
-}
 
 // dz without the dropout's scale (so that, where act' is 0 or 1, it is dy or zero and loses nothing in bf16) and sums of its
 // rows.  A lane takes a chunk of columns, 16 bytes, of the gate and of the linear part; `lanes` lanes of a block share a row
@@ -113,25 +23,9 @@ struct DzArgs {
     Drop drop;
 };
 
-template <typename T> struct DzChunk;
-template <> struct DzChunk<bf16> {
-    static constexpr int n = 8;
-    static __device__ __forceinline__ void load(const void *p, int64_t at, float *v) { Eight<bf16>::load((const bf16 *)p + at, v); }
-    static __device__ __forceinline__ void store(void *p, int64_t at, const float *v) { Eight<bf16>::store((bf16 *)p + at, v); }
-};
-template <> struct DzChunk<float> {
-    static constexpr int n = 4;
-    static __device__ __forceinline__ void load(const void *p, int64_t at, float *v) {
-        *(float4 *)v = *(const float4 *)((const float *)p + at);
-    }
-    static __device__ __forceinline__ void store(void *p, int64_t at, const float *v) {
-        *(float4 *)((float *)p + at) = *(const float4 *)v;
-    }
-};
-
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
-    typedef DzChunk<T> C;
+    typedef Row16<T> C;
     constexpr int n = C::n, NP = GATED ? 2 : 1;
     __shared__ float sums[256][NP * n + 1];
     const int tid = threadIdx.x, line = tid / a.lanes, lines = 256 / a.lanes;
@@ -191,44 +85,57 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
     }
 }
 
-// The parts' sums of dW and, in the blocks behind, of db, in the order of the parts.
+// Sums of parts, in their order: of dx, of dW and, by lines of blocks behind, of db.
+struct LinearSum {
+    const float *part;
+    void *out;
+    int64_t elements;
+    int splits, blocks;
+};
 struct LinearJoin {
-    const float *dW_part;
-    void *dW;
-    int64_t elements;              // of dW
-    int splits;
-    int dW_blocks;
+    LinearSum dx, dW;
     const float *db_part;
     float *db;
     int64_t db_parts;
     int cols;
     float scale;
 };
-constexpr int kJoinCols = 32;
-template <typename T> __global__ __launch_bounds__(1024) void linear_join_kernel(LinearJoin a) {
-    typedef DzChunk<T> C;
-    if ((int)blockIdx.x < a.dW_blocks) {
-        const int64_t at = ((int64_t)blockIdx.x * 1024 + threadIdx.x) * C::n;
-        if (at >= a.elements) return;
-        float sum[C::n] = {};
+constexpr int kJoinThreads = 1024, kJoinCols = 32;
+
+template <int n> __device__ __forceinline__ void add_parts(const float *part, int splits, int64_t stride, float *sum) {
+#pragma unroll
+    for (int m = 0; m < n; ++m) sum[m] = 0.f;
 #pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) {
-            const float *from = a.dW_part + s * a.elements + at;
+    for (int s = 0; s < splits; ++s) {
+        const float *from = part + s * stride;
 #pragma unroll
-            for (int m = 0; m < C::n; m += 4) {
-                const float4 x = *(const float4 *)(from + m);
-                sum[m] += x.x; sum[m + 1] += x.y; sum[m + 2] += x.z; sum[m + 3] += x.w;
-            }
+        for (int m = 0; m < n; m += 4) {
+            const float4 x = *(const float4 *)(from + m);
+            sum[m] += x.x; sum[m + 1] += x.y; sum[m + 2] += x.z; sum[m + 3] += x.w;
         }
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(kJoinThreads) void linear_join_kernel(LinearJoin a) {
+    constexpr int n = Row16<T>::n;
+    int b = blockIdx.x;
+    if (b < a.dx.blocks + a.dW.blocks) {
+        const LinearSum &w = b < a.dx.blocks ? a.dx : a.dW;
+        if (b >= a.dx.blocks) b -= a.dx.blocks;
+        const int64_t at = ((int64_t)b * kJoinThreads + threadIdx.x) * n;
+        if (at >= w.elements) return;
+        float sum[n];
+        add_parts<n>(w.part + at, w.splits, w.elements, sum);
 #pragma unroll
-        for (int m = 0; m < C::n; ++m) sum[m] *= a.scale;
-        C::store(a.dW, at, sum);
+        for (int m = 0; m < n; ++m) sum[m] *= a.scale;
+        Row16<T>::store(w.out, at, sum);
         return;
     }
-    constexpr int kLines = 1024 / kJoinCols;
+    b -= a.dx.blocks + a.dW.blocks;
+    constexpr int kLines = kJoinThreads / kJoinCols;
     __shared__ double sums[kLines][kJoinCols + 1];
     const int col = threadIdx.x % kJoinCols, line = threadIdx.x / kJoinCols;
-    const int p = ((int)blockIdx.x - a.dW_blocks) * kJoinCols + col;
+    const int p = b * kJoinCols + col;
     double sum = 0.;
     if (p < a.cols)
 #pragma unroll 4
@@ -240,6 +147,117 @@ template <typename T> __global__ __launch_bounds__(1024) void linear_join_kernel
         for (int l = 0; l < kLines; ++l) sum += sums[l][col];
         a.db[p] = (float)(sum * a.scale);
     }
+}
+
+// The forward pass behind several parts of k: their sums and the epilogue.
+template <typename T, int ACT> __global__ __launch_bounds__(256) void linear_finish_kernel(LinearArgs a, int splits) {
+    constexpr int n = Row16<T>::n;
+    constexpr bool GATED = ACT == SW_ACT_GEGLU;
+    const uint32_t chunks = (uint32_t)a.Pdim / n;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, q = i / chunks;
+    if (q >= a.Qdim) return;
+    const int p = (int)(i - q * chunks) * n;
+    const int64_t cols = GATED ? 2 * (int64_t)a.Pdim : a.Pdim;
+    const float *from = a.part + q * cols + p;
+    float v[n], lin[n];
+    add_parts<n>(from, splits, a.Qdim * cols, v);
+    if (GATED) add_parts<n>(from + a.Pdim, splits, a.Qdim * cols, lin);
+    linear_emit<T, ACT>(a, q, p, v, lin);
+}
+template <typename T> static hipError_t linear_finish(const LinearArgs &a, int splits, hipStream_t s) {
+    ProfScope ps("linear_finish", s);
+    const dim3 grid((unsigned)ceil_div(a.Qdim * (a.Pdim / Row16<T>::n), 256));
+    auto kern = a.act == SW_ACT_RELU    ? linear_finish_kernel<T, SW_ACT_RELU>
+                : a.act == SW_ACT_GELU  ? linear_finish_kernel<T, SW_ACT_GELU>
+                : a.act == SW_ACT_GEGLU ? linear_finish_kernel<T, SW_ACT_GEGLU>
+                                        : linear_finish_kernel<T, SW_ACT_NONE>;
+    hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a, splits);
+    return hipGetLastError();
+}
+
+// ---- how a product is cut ---------------------------------------------------------------------
+// Per kind of tile: k of a step; us of a step per block of a CU (of the blocks that share it, one after the other) and of
+// a step at least; us of a block's start and end; blocks that a CU holds.  Measured with products of 4 to 64 steps.
+struct LinearModel {
+    int tile, bk;
+    double step, least, once;
+    int resident;
+};
+static const LinearModel kBf16Models[] = {{256, 64, 1.45, 1.45, 10., 1}, {128, 64, 0.52, 0.75, 8., 2}};
+static const LinearModel kF32Models[] = {{64, 32, 0.45, 0.6, 5., 4}};
+constexpr int kCUs = 256;
+constexpr double kJoinUs = 4., kJoinGbs = 4000.;   // of a launch that adds up parts, and its traffic's rate
+
+static double join_us(int splits, double elements) {
+    return splits > 1 ? kJoinUs + splits * elements * 8e-3 / kJoinGbs : 0.;
+}
+static LinearCut cut_of(int64_t k, int splits, int bk) {
+    const int64_t split_k = ceil_div(ceil_div(k, splits), bk) * bk;
+    return LinearCut{(int)ceil_div(k, split_k), split_k};
+}
+
+LinearPlan plan_linear(const switch_linear_config *cfg, bool backward) {
+    const int64_t M = cfg->M, K = cfg->K, Nz = linear_columns(cfg);
+    LinearPlan plan{64, {1, backward ? Nz : K}, {1, M}};
+    if (M == 0) return plan;
+    if (!backward && linear_few_rows(cfg)) return LinearPlan{0, linear_few_cut(cfg), {1, M}};
+    const bool bf = cfg->act_dtype == SW_BF16;
+    // the rows of a part of dW: what a descriptor of 2 GB spans
+    const int64_t widest = (K > Nz ? K : Nz) * (bf ? 2 : 4), most_k = (int64_t)0x7fffffff / widest / 64 * 64;
+    static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    double best = 1e30;
+    const LinearModel *models = bf ? kBf16Models : kF32Models;
+    for (int i = 0; i < (bf ? 2 : 1); ++i) {
+        const LinearModel &m = models[i];
+        const double tx = (double)ceil_div(M, m.tile) * ceil_div(backward ? K : Nz, m.tile);
+        const int64_t kx = backward ? Nz : K;
+        for (int sx : kSplits) {
+            // (parts of y or dx only while its tiles leave CUs idle; four steps at least)
+            if (sx > 1 && (tx * sx > 2 * kCUs || kx < (int64_t)sx * 4 * m.bk)) break;
+            const LinearCut x = cut_of(kx, sx, m.bk);
+            const double steps_x = (double)ceil_div(x.split_k, m.bk), items_x = tx * x.splits;
+            auto time_of = [&](double per_cu, double steps) {
+                return ceil(per_cu / m.resident) * m.once + steps * fmax(per_cu * m.step, m.least);
+            };
+            if (!backward) {
+                const double us = time_of(ceil(items_x / kCUs), steps_x) + join_us(x.splits, (double)M * Nz);
+                if (us < best) {
+                    best = us;
+                    plan = LinearPlan{m.tile, x, {1, M}};
+                }
+                continue;
+            }
+            const double tw = (double)ceil_div(K, m.tile) * ceil_div(Nz, m.tile);
+            bool found = false;   // (a cut whose parts a descriptor spans)
+            for (int sw : kSplits) {
+                if (found && (tw * sw > 4 * kCUs * m.resident || M < (int64_t)sw * 4 * m.bk)) break;
+                LinearCut w = cut_of(M, sw, m.bk);
+                if (w.split_k > most_k) {
+                    if (sw < 64) continue;
+                    w = LinearCut{(int)ceil_div(M, most_k), most_k};
+                }
+                found = true;
+                const double steps_w = (double)ceil_div(w.split_k, m.bk), items_w = tw * w.splits;
+                // dx's tiles, then dW's on what they leave idle: whole blocks
+                const double bx = steps_x * m.step + m.once / m.resident, bw = steps_w * m.step + m.once / m.resident;
+                const double rounds = floor(items_x / kCUs), over = items_x - rounds * kCUs, t0 = rounds * bx;
+                double end = fmax(t0 + (over > 0 ? bx : 0.), (items_x * bx + items_w * bw) / kCUs);
+                for (int j = 0; j < 16; ++j) {
+                    const double na = floor(fmax(end - t0 - bx, 0.) / bw + 1e-9), nb = floor((end - t0) / bw + 1e-9);
+                    if (over * na + (kCUs - over) * nb >= items_w) break;
+                    const double a = t0 + bx + (na + 1.) * bw, b = t0 + (nb + 1.) * bw;
+                    end = over > 0 && a < b ? a : b;
+                }
+                end = fmax(end, fmax(steps_x, steps_w) * m.least + m.once);
+                const double us = end + join_us(x.splits, (double)M * K) + join_us(w.splits, (double)K * Nz);
+                if (us < best) {
+                    best = us;
+                    plan = LinearPlan{m.tile, x, w};
+                }
+            }
+        }
+    }
+    return plan;
 }
 
 static int check_linear(const switch_linear_config *cfg) {
@@ -258,7 +276,7 @@ static int check_linear(const switch_linear_config *cfg) {
 }
 
 struct LinearLayout {
-    size_t dz, db_part, dW_part, total;
+    size_t dz, db_part, x_part, w_part, total;
     bool own_dz;                   // dz is not dy itself
     int lanes;                     // of linear_dz_kernel
     int64_t db_parts;
@@ -268,10 +286,8 @@ static LinearLayout linear_layout(const switch_linear_config *cfg, bool backward
     LinearLayout l{};
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
-    const bool bf = cfg->act_dtype == SW_BF16;
-    const int64_t elt = bf ? 2 : 4, cols = linear_columns(cfg);
-    if (bf) l.plan = plan_linear_bf16(cfg, backward);
-    else l.plan = LinearPlan{0, 1, cfg->M};
+    const int64_t elt = cfg->act_dtype == SW_BF16 ? 2 : 4, cols = linear_columns(cfg);
+    l.plan = plan_linear(cfg, backward);
     if (backward) {
         l.own_dz = cfg->activation != SW_ACT_NONE || drop_of(cfg->dropout, 0).on;
         const int64_t chunks = cfg->N * elt / 16;
@@ -280,18 +296,11 @@ static LinearLayout linear_layout(const switch_linear_config *cfg, bool backward
         l.db_parts = ceil_div(cfg->M, 256 / l.lanes * kDzSteps);
         l.dz = take(l.own_dz ? (size_t)cfg->M * cols * elt : 0);
         l.db_part = take((size_t)l.db_parts * cols * 4);
-        l.dW_part = take(l.plan.splits > 1 ? (size_t)l.plan.splits * cfg->K * cols * 4 : 0);
+        l.w_part = take(l.plan.w.splits > 1 ? (size_t)l.plan.w.splits * cfg->K * cols * 4 : 0);
     }
+    l.x_part = take(l.plan.x.splits > 1 ? (size_t)l.plan.x.splits * cfg->M * (backward ? cfg->K : cols) * 4 : 0);
     l.total = cfg->M ? off : 0;
     return l;
-}
-
-static hipError_t launch_linear_f32(const char *name, LinearKind kind, const LinearArgs &a, hipStream_t s) {
-    ProfScope ps(name, s);
-    const dim3 grid((unsigned)ceil_div(a.Qdim, kLinTile), (unsigned)ceil_div(a.Pdim, kLinTile));
-    if (a.gated) hipLaunchKernelGGL((linear_kernel<float, true>), grid, dim3(256), 0, s, a, (int)kind);
-    else hipLaunchKernelGGL((linear_kernel<float, false>), grid, dim3(256), 0, s, a, (int)kind);
-    return hipGetLastError();
 }
 
 static bool linear_workspace_ok(const LinearLayout &l, const void *workspace, size_t bytes) {
@@ -314,7 +323,7 @@ int switch_linear_workspace_size(const switch_linear_config *cfg, int backward, 
 
 int switch_linear(const switch_linear_config *cfg, const void *x, const void *W, const float *bias,
                   const void *residual, void *y, void *z, void *workspace, size_t workspace_bytes, void *hip_stream) {
-    const int st = check_linear(cfg);
+    int st = check_linear(cfg);
     if (st != SW_OK) return st;
     if (cfg->M == 0) return SW_OK;
     if (!x || !W || !y) return SW_ERR_NULL;
@@ -322,17 +331,26 @@ int switch_linear(const switch_linear_config *cfg, const void *x, const void *W,
         return SW_ERR_ALIGN;
     const LinearLayout l = linear_layout(cfg, false);
     if (!linear_workspace_ok(l, workspace, workspace_bytes)) return SW_ERR_WORKSPACE;
+    const bool bf = cfg->act_dtype == SW_BF16;
     LinearArgs a{};
     a.Q = x; a.ldq = (int)cfg->K;
     a.P = W; a.ldp = (int)linear_columns(cfg);
     a.Qdim = cfg->M; a.Kdim = cfg->K; a.Pdim = (int)cfg->N;
     a.bias = bias; a.residual = residual; a.C = y; a.z = z;
+    a.part = (float *)((char *)workspace + l.x_part);
     a.act = cfg->activation;
     a.gated = cfg->activation == SW_ACT_GEGLU;
     a.scale = 1.f;
     a.drop = drop_of(cfg->dropout, cfg->seed);
     hipStream_t s = (hipStream_t)hip_stream;
-    return status_of(cfg->act_dtype == SW_BF16 ? launch_linear_bf16(l.plan, a, s) : launch_linear_f32("linear", LINEAR_FWD, a, s));
+    {
+        ProfScope ps("linear", s);
+        st = status_of(l.plan.tile == 0 ? launch_linear_few(cfg->act_dtype, l.plan, a, s)
+                       : bf             ? launch_linear_bf16(l.plan, a, s)
+                                        : launch_linear_f32(l.plan, a, s));
+    }
+    if (st || l.plan.x.splits == 1) return st;
+    return status_of(bf ? linear_finish<bf16>(a, l.plan.x.splits, s) : linear_finish<float>(a, l.plan.x.splits, s));
 }
 
 int switch_linear_backward(const switch_linear_config *cfg, const void *dy, const void *x, const void *W, const void *z,
@@ -376,35 +394,33 @@ int switch_linear_backward(const switch_linear_config *cfg, const void *dy, cons
     ax.Q = dz; ax.ldq = (int)cols;
     ax.P = W; ax.ldp = (int)cols;
     ax.Qdim = cfg->M; ax.Kdim = cols; ax.Pdim = (int)cfg->K;
-    ax.C = dx;
+    ax.C = dx; ax.part = (float *)(ws + l.x_part);
     aw.Q = x; aw.ldq = (int)cfg->K;
     aw.P = dz; aw.ldp = (int)cols;
     aw.Qdim = cfg->K; aw.Kdim = cfg->M; aw.Pdim = (int)cols;
-    aw.C = dW; aw.part = (float *)(ws + l.dW_part);
-    if (bf) {
-        if ((dx || dW) && (st = status_of(launch_linear_backward_bf16(l.plan, dx ? &ax : nullptr, dW ? &aw : nullptr, s)))) return st;
-    } else {
-        if (dx && (st = status_of(launch_linear_f32("linear_dx", LINEAR_DX, ax, s)))) return st;
-        if (dW && (st = status_of(launch_linear_f32("linear_dW", LINEAR_DW, aw, s)))) return st;
+    aw.C = dW; aw.part = (float *)(ws + l.w_part);
+    if (dx || dW) {
+        ProfScope ps("linear_backward", s);
+        auto launch = bf ? launch_linear_backward_bf16 : launch_linear_backward_f32;
+        if ((st = status_of(launch(l.plan, dx ? &ax : nullptr, dW ? &aw : nullptr, s)))) return st;
     }
-    const bool join_dW = dW && l.plan.splits > 1;
-    if (join_dW || db) {
-        ProfScope ps("linear_join", s);
-        LinearJoin j{};
-        j.dW_part = aw.part; j.dW = dW;
-        j.elements = cfg->K * cols;
-        j.splits = l.plan.splits;
-        j.dW_blocks = join_dW ? (int)ceil_div(j.elements, 1024 * (bf ? 8 : 4)) : 0;
-        j.db_part = (const float *)(ws + l.db_part); j.db = db;
-        j.db_parts = l.db_parts;
-        j.cols = (int)cols;
-        j.scale = drop.scale;
-        const dim3 grid((unsigned)(j.dW_blocks + (db ? ceil_div(cols, kJoinCols) : 0)));
-        if (bf) hipLaunchKernelGGL(linear_join_kernel<bf16>, grid, dim3(1024), 0, s, j);
-        else hipLaunchKernelGGL(linear_join_kernel<float>, grid, dim3(1024), 0, s, j);
-        st = status_of(hipGetLastError());
-    }
-    return st;
+    LinearJoin j{};
+    auto sum = [&](const LinearArgs &a, int splits) {
+        const int64_t elements = a.Qdim * a.Pdim;
+        return LinearSum{a.part, a.C, elements, splits, (int)ceil_div(elements, kJoinThreads * (bf ? 8 : 4))};
+    };
+    if (dx && l.plan.x.splits > 1) j.dx = sum(ax, l.plan.x.splits);
+    if (dW && l.plan.w.splits > 1) j.dW = sum(aw, l.plan.w.splits);
+    if (!j.dx.blocks && !j.dW.blocks && !db) return SW_OK;
+    ProfScope ps("linear_join", s);
+    j.db_part = (const float *)(ws + l.db_part); j.db = db;
+    j.db_parts = l.db_parts;
+    j.cols = (int)cols;
+    j.scale = drop.scale;
+    const dim3 grid((unsigned)(j.dx.blocks + j.dW.blocks + (db ? ceil_div(cols, kJoinCols) : 0)));
+    if (bf) hipLaunchKernelGGL(linear_join_kernel<bf16>, grid, dim3(kJoinThreads), 0, s, j);
+    else hipLaunchKernelGGL(linear_join_kernel<float>, grid, dim3(kJoinThreads), 0, s, j);
+    return status_of(hipGetLastError());
 }
 
 }  // extern "C"

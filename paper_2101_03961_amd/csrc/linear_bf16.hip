@@ -4,8 +4,6 @@
 // blocks, one per CU: the loads run one (Q) and two (P) steps of 64 k ahead of the products, over the end of a tile into the
 // block's next one, so that a tile's first loads and its stores overlap with products.  Small ones, 128 x 128 in four waves, two
 // blocks per CU, for products with too few large tiles.
-#include <math.h>
-
 #include "linear.h"
 #include "rows_operands.h"
 
@@ -34,51 +32,6 @@ template <int IP, int WP, int NW> struct GatedTrans : RowsTrans<32 * IP * WP, NW
     }
 };
 
-struct LinearTiles {
-    int tiles_q, tiles_p;
-    int splits;
-    int64_t split_k;
-};
-
-// A tile's place: item n of the product.  Items of a part of k are neighbours, in bands of eight row tiles, so that
-// those that run on an XCD at a time, 32 in a row, share their operands in its L2.
-struct LinearPlace {
-    int64_t q0, k0;
-    int p0, split, klim;
-};
-template <int QB, int OUTP, LinearKind KIND>
-__device__ __forceinline__ LinearPlace linear_place(const LinearArgs &a, const LinearTiles &t, int n) {
-    LinearPlace at;
-    const int tiles = t.tiles_q * t.tiles_p;
-    at.split = KIND == LINEAR_DW ? n / tiles : 0;
-    n -= at.split * tiles;
-    constexpr int kBand = 8;
-    const int band = n / (kBand * t.tiles_p), rows = min(kBand, t.tiles_q - band * kBand);
-    n -= band * kBand * t.tiles_p;
-    const int pt = n / rows;
-    at.q0 = (int64_t)(band * kBand + (n - pt * rows)) * QB;
-    at.p0 = pt * OUTP;
-    at.k0 = at.split * t.split_k;
-    at.klim = (int)(KIND == LINEAR_DW && a.Kdim - at.k0 > t.split_k ? t.split_k : a.Kdim - at.k0);
-    return at;
-}
-
-// The operands' loads of a tile.  (Descriptors span 32 bits: W is below 2 GB; a tile's rows of x and dz, and a part's rows of
-// both, begin at the base.)
-template <LinearKind KIND, bool GATED, typename OP>
-__device__ __forceinline__ void linear_init_p(OP &op, const LinearArgs &a, const LinearPlace &at, int lane, int wave) {
-    if constexpr (GATED) op.init_gated((const bf16 *)a.P, a.ldp, at.p0, a.Pdim, at.klim, lane, wave);
-    else
-        op.init((const bf16 *)a.P + (KIND == LINEAR_DW ? (size_t)at.k0 * a.ldp : 0), a.ldp, at.p0, a.Pdim, at.klim, lane, wave);
-}
-template <LinearKind KIND, int QB, typename OQ>
-__device__ __forceinline__ void linear_init_q(OQ &oq, const LinearArgs &a, const LinearPlace &at, int lane, int wave) {
-    if constexpr (KIND == LINEAR_DW)
-        oq.init((const bf16 *)a.Q + (size_t)at.k0 * a.ldq, a.ldq, (int)at.q0, (int)a.Qdim, at.klim, lane, wave);
-    else
-        oq.init((const bf16 *)a.Q + (size_t)at.q0 * a.ldq, a.ldq, 0, (int)min(a.Qdim - at.q0, (int64_t)QB), at.klim, lane, wave);
-}
-
 // Epilogue of a wave: 16 rows at a time through 2 KB IP of LDS of its own, as fp32, so that a lane has eight consecutive
 // columns (of the gate and the linear part) and rows leave in whole segments.  The 16-byte chunks of a row trade places by
 // the row, so that neither side has bank conflicts.
@@ -95,12 +48,8 @@ __device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const Linea
     const int rows = (int)min(a.Qdim - at.q0, (int64_t)0x7fffffff) - wq * IQ * 32;   // of the wave
     const int64_t q0 = at.q0 + wq * IQ * 32;
     const bool in = p < a.Pdim;
-    float bu[8], bv[8];
-    if (KIND == LINEAR_FWD && a.bias && in) {
-        Eight<float>::load(a.bias + p, bu);
-        if (GATED) Eight<float>::load(a.bias + a.Pdim + p, bv);
-    }
-    const int64_t Nz = GATED ? 2 * (int64_t)a.Pdim : a.Pdim;
+    LinearColumns<bf16, ACT> col;
+    if (KIND == LINEAR_FWD && in) col.load(a, p);
 #pragma unroll
     for (int j = 0; j < 2 * IQ; ++j) {
         if (j * 16 >= rows) break;
@@ -127,38 +76,20 @@ __device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const Linea
                 *(f32x4 *)(lin + 4) = chunk(2 * c + 1 + kCols / 4);
             }
             if (row >= rows || !in) continue;
-            const int64_t q = q0 + row, out = q * a.Pdim + p;
-            if (KIND == LINEAR_DW && t.splits > 1) {
-                Eight<float>::store(a.part + ((int64_t)at.split * a.Qdim * a.Pdim + out), v);
-                continue;
-            }
-            if (KIND != LINEAR_FWD) {
-#pragma unroll
-                for (int m = 0; m < 8; ++m) v[m] *= a.scale;
-            } else {
-                if (a.bias) {
-#pragma unroll
-                    for (int m = 0; m < 8; ++m) {
-                        v[m] += bu[m];
-                        if (GATED) lin[m] += bv[m];
-                    }
-                }
-                if (a.z) {
-                    Eight<bf16>::store((bf16 *)a.z + q * Nz + p, v);
-                    if (GATED) Eight<bf16>::store((bf16 *)a.z + q * Nz + a.Pdim + p, lin);
-                }
-#pragma unroll
-                for (int m = 0; m < 8; ++m) v[m] = linear_act(ACT, v[m], GATED ? lin[m] : 0.f);
-                if (a.drop.on) {
-                    drop_apply<8>(a.drop, (uint64_t)out, v);
-#pragma unroll
-                    for (int m = 0; m < 8; ++m) v[m] *= a.drop.scale;
-                }
+            const int64_t q = q0 + row;
+            if (t.cut.splits > 1) {
+                linear_store_part<8, GATED>(a, at.split, q, p, v, lin);
+            } else if (KIND == LINEAR_FWD) {
+                float r8[8];
                 if (a.residual)
 #pragma unroll
-                    for (int m = 0; m < 8; ++m) v[m] += (float)res[x][m];
+                    for (int m = 0; m < 8; ++m) r8[m] = (float)res[x][m];
+                linear_emit<bf16, ACT>(a, col, q, p, v, lin, r8);
+            } else {
+#pragma unroll
+                for (int m = 0; m < 8; ++m) v[m] *= a.scale;
+                Eight<bf16>::store((bf16 *)a.C + q * a.Pdim + p, v);
             }
-            Eight<bf16>::store((bf16 *)a.C + out, v);
         }
     }
 }
@@ -211,15 +142,15 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wp = wave % WP, wq = wave / WP;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    const LinearPlace at = linear_place<S::QB, S::OUTP, KIND>(a, t, n);
+    const LinearPlace at = linear_place(a, t, n, S::QB, S::OUTP);
     typename S::P op;
     typename S::Q oq;
     constexpr int kLoadsP = S::P::kLoads, kLoadsQ = S::Q::kLoads;
     static_assert(kLoadsP + kLoadsQ == 16, "a load per group of products");
     op.init_frag16(lane, wp * 32 * IP);
     oq.init_frag16(lane, wq * 32 * IQ);
-    linear_init_p<KIND, GATED>(op, a, at, lane, wave);
-    linear_init_q<KIND, S::QB>(oq, a, at, lane, wave);
+    linear_init_p<KIND, GATED, bf16>(op, a, at, lane, wave);
+    linear_init_q<KIND, S::QB, bf16>(oq, a, at, lane, wave);
     f32x4 acc[2 * IP][2 * IQ];
 #pragma unroll
     for (int i = 0; i < 2 * IP; ++i)
@@ -306,15 +237,10 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
     linear_epilogue<IP, IQ, WQ, KIND, ACT>(a, t, at, acc, lds + wave * S::kTurn, lane, wp, wq);
 }
 
-// item of a block when the blocks of an XCD (b mod 8) take neighbouring ones
-__device__ __forceinline__ int linear_item(int b, int total) {
-    return (b & 7) * ((total + 7) >> 3) + (b >> 3);
-}
-
 template <int ACT>
 __global__ __launch_bounds__(256, 1) void linear_fwd_large_kernel(LinearArgs a, LinearTiles t) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int total = t.tiles_q * t.tiles_p, n = linear_item(blockIdx.x, total);
+    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(blockIdx.x, total);
     if (n < total) linear_large<LINEAR_FWD, ACT>(a, t, lds, n);
 }
 
@@ -322,10 +248,10 @@ __global__ __launch_bounds__(256, 1) void linear_bwd_large_kernel(LinearArgs dx,
                                                                   int dx_blocks) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     if ((int)blockIdx.x < dx_blocks) {
-        const int total = tx.tiles_q * tx.tiles_p, n = linear_item(blockIdx.x, total);
+        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(blockIdx.x, total);
         if (n < total) linear_large<LINEAR_DX, SW_ACT_NONE>(dx, tx, lds, n);
     } else {
-        const int total = tw.tiles_q * tw.tiles_p * tw.splits, n = linear_item(blockIdx.x - dx_blocks, total);
+        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(blockIdx.x - dx_blocks, total);
         if (n < total) linear_large<LINEAR_DW, SW_ACT_NONE>(dW, tw, lds, n);
     }
 }
@@ -340,13 +266,13 @@ __device__ __forceinline__ void linear_small(const LinearArgs &a, const LinearTi
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wp = wave % WP, wq = wave / WP;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    const LinearPlace at = linear_place<S::QB, S::OUTP, KIND>(a, t, n);
+    const LinearPlace at = linear_place(a, t, n, S::QB, S::OUTP);
     typename S::P op;
     typename S::Q oq;
     op.init_frag16(lane, wp * 32 * IP);
     oq.init_frag16(lane, wq * 32 * IQ);
-    linear_init_p<KIND, GATED>(op, a, at, lane, wave);
-    linear_init_q<KIND, S::QB>(oq, a, at, lane, wave);
+    linear_init_p<KIND, GATED, bf16>(op, a, at, lane, wave);
+    linear_init_q<KIND, S::QB, bf16>(oq, a, at, lane, wave);
     f32x4 acc[2 * IP][2 * IQ];
 #pragma unroll
     for (int i = 0; i < 2 * IP; ++i)
@@ -387,7 +313,7 @@ __device__ __forceinline__ void linear_small(const LinearArgs &a, const LinearTi
 template <int ACT>
 __global__ __launch_bounds__(256, 2) void linear_fwd_small_kernel(LinearArgs a, LinearTiles t) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int total = t.tiles_q * t.tiles_p, n = linear_item(blockIdx.x, total);
+    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(blockIdx.x, total);
     if (n < total) linear_small<LINEAR_FWD, ACT>(a, t, lds, n);
 }
 
@@ -395,10 +321,10 @@ __global__ __launch_bounds__(256, 2) void linear_bwd_small_kernel(LinearArgs dx,
                                                                   int dx_blocks) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     if ((int)blockIdx.x < dx_blocks) {
-        const int total = tx.tiles_q * tx.tiles_p, n = linear_item(blockIdx.x, total);
+        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(blockIdx.x, total);
         if (n < total) linear_small<LINEAR_DX, SW_ACT_NONE>(dx, tx, lds, n);
     } else {
-        const int total = tw.tiles_q * tw.tiles_p * tw.splits, n = linear_item(blockIdx.x - dx_blocks, total);
+        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(blockIdx.x - dx_blocks, total);
         if (n < total) linear_small<LINEAR_DW, SW_ACT_NONE>(dW, tw, lds, n);
     }
 }
@@ -407,98 +333,20 @@ __global__ __launch_bounds__(256, 2) void linear_bwd_small_kernel(LinearArgs dx,
 constexpr int kLargeTile = 256, kSmallTile = 128;
 constexpr int kLargeLds = 5 * kLargeTile * BK * 2, kSmallLds = 2 * 2 * kSmallTile * BK * 2;
 static_assert(kLargeLds == 160 * 1024, "all of a CU's");
-constexpr int kCUs = 256;
-
-// us of a step of 64 k and of a tile's start and end, all CUs busy: large tiles one at a time per CU, small ones two
-constexpr double kLargeStep = 1.6, kLargeOnce = 6., kSmallStep = 1.03, kSmallOnce = 6.;
-
-static double rounds_us(double tiles, double slots, double us) { return ceil(tiles / slots) * us; }
-
-LinearPlan plan_linear_bf16(const switch_linear_config *cfg, bool backward) {
-    const int64_t M = cfg->M, K = cfg->K, Nz = linear_columns(cfg);
-    LinearPlan plan{0, 1, M};
-    if (M == 0) return plan;
-    if (!backward) {
-        const double steps = (double)ceil_div(K, BK);
-        const double large = rounds_us((double)(ceil_div(M, 256) * ceil_div(Nz, 256)), kCUs, steps * kLargeStep + kLargeOnce);
-        const double small = rounds_us((double)(ceil_div(M, 128) * ceil_div(Nz, 128)), 2 * kCUs, steps * kSmallStep + kSmallOnce);
-        plan.tile = large <= small ? kLargeTile : kSmallTile;
-        return plan;
-    }
-    // parts of k: at least what the descriptors ask for; more where the tiles leave CUs idle.  A part costs its sums'
-    // store and load.
-    const int64_t widest = K > Nz ? K : Nz, most_k = ((int64_t)0x7fffffff / (2 * widest)) / BK * BK;
-    double best = 1e30;
-    for (int tile : {kLargeTile, kSmallTile}) {
-        const double step = tile == kLargeTile ? kLargeStep : kSmallStep, once = tile == kLargeTile ? kLargeOnce : kSmallOnce;
-        const double slots = tile == kLargeTile ? kCUs : 2 * kCUs;
-        const double tx = (double)(ceil_div(M, tile) * ceil_div(K, tile)), tw = (double)(ceil_div(K, tile) * ceil_div(Nz, tile));
-        const double dx_us = ceil_div(Nz, BK) * step + once;
-        int64_t last = 0;
-        for (int s = 1; s <= 64; ++s) {
-            const int64_t split_k = ceil_div(ceil_div(M, s), BK) * BK, splits = ceil_div(M, split_k);
-            if (split_k > most_k || splits == last) continue;
-            last = splits;
-            const double dw_us = split_k / BK * step + once;
-            // list scheduling: dx's tiles first
-            const double full = floor(tx / slots), over = tx - full * slots, t0 = full * dx_us;
-            const double items = tw * (double)splits;
-            // smallest end at which the blocks have room for the items
-            double end = t0 + (over > 0 ? dx_us : 0.);
-            for (int i = 0; i < 4096; ++i) {
-                const double room = over * floor(fmax(end - t0 - dx_us, 0.) / dw_us + 1e-9) + (slots - over) * floor((end - t0) / dw_us + 1e-9);
-                if (room >= items) break;
-                const double a = t0 + dx_us + (floor(fmax(end - t0 - dx_us, 0.) / dw_us + 1e-9) + 1.) * dw_us;
-                const double b = t0 + (floor((end - t0) / dw_us + 1e-9) + 1.) * dw_us;
-                end = over > 0 && a < b ? a : b;
-            }
-            const double join = splits > 1 ? 4. + (double)splits * K * Nz * 8. / 4e6 : 0.;
-            if (end + join < best) {
-                best = end + join;
-                plan.tile = tile;
-                plan.splits = (int)splits;
-                plan.split_k = split_k;
-            }
-        }
-        if (best > 1e29) {   // (more rows than 64 parts of the widest descriptor hold)
-            plan.tile = tile;
-            plan.split_k = most_k;
-            plan.splits = (int)ceil_div(M, most_k);
-        }
-    }
-    return plan;
-}
-
-static LinearTiles linear_tiles(const LinearArgs &a, int tile, const LinearPlan &plan, bool dW) {
-    LinearTiles t;
-    t.tiles_q = (int)ceil_div(a.Qdim, tile);
-    t.tiles_p = (int)ceil_div(a.Pdim, a.gated ? tile / 2 : tile);
-    t.splits = dW ? plan.splits : 1;
-    t.split_k = dW ? plan.split_k : a.Kdim;
-    return t;
-}
-
-template <typename F> static hipError_t with_lds(PerDeviceOnce &once, F kernel, int bytes) {
-    return once_per_device(once, [&] {
-        return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    });
-}
 
 template <int ACT> static hipError_t linear_fwd_bf16(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
     const bool large = plan.tile == kLargeTile;
-    const LinearTiles t = linear_tiles(a, plan.tile, plan, false);
-    const int64_t blocks = ceil_div((int64_t)t.tiles_q * t.tiles_p, 8) * 8;
+    const LinearTiles t = linear_tiles(a, plan.tile, plan.x);
     auto kern = large ? linear_fwd_large_kernel<ACT> : linear_fwd_small_kernel<ACT>;
     static PerDeviceOnce once[2];
     const int lds = large ? kLargeLds : kSmallLds;
     const hipError_t err = with_lds(once[large], kern, lds);
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(256), lds, s, a, t);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(linear_items(t), 8) * 8)), dim3(256), lds, s, a, t);
     return hipGetLastError();
 }
 
 hipError_t launch_linear_bf16(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
-    ProfScope ps("linear", s);
     switch (a.act) {
     case SW_ACT_RELU: return linear_fwd_bf16<SW_ACT_RELU>(plan, a, s);
     case SW_ACT_GELU: return linear_fwd_bf16<SW_ACT_GELU>(plan, a, s);
@@ -508,14 +356,11 @@ hipError_t launch_linear_bf16(const LinearPlan &plan, const LinearArgs &a, hipSt
 }
 
 hipError_t launch_linear_backward_bf16(const LinearPlan &plan, const LinearArgs *dx, const LinearArgs *dW, hipStream_t s) {
-    ProfScope ps("linear_backward", s);
     const bool large = plan.tile == kLargeTile;
     const LinearArgs none{};
     const LinearArgs &ax = dx ? *dx : none, &aw = dW ? *dW : none;
-    const LinearTiles tx = dx ? linear_tiles(ax, plan.tile, plan, false) : LinearTiles{};
-    const LinearTiles tw = dW ? linear_tiles(aw, plan.tile, plan, true) : LinearTiles{};
-    const int64_t bx = ceil_div((int64_t)tx.tiles_q * tx.tiles_p, 8) * 8;
-    const int64_t bw = ceil_div((int64_t)tw.tiles_q * tw.tiles_p * tw.splits, 8) * 8;
+    const LinearTiles tx = linear_tiles(ax, plan.tile, plan.x), tw = linear_tiles(aw, plan.tile, plan.w);
+    const int64_t bx = ceil_div(linear_items(tx), 8) * 8, bw = ceil_div(linear_items(tw), 8) * 8;
     auto kern = large ? linear_bwd_large_kernel : linear_bwd_small_kernel;
     static PerDeviceOnce once[2];
     const int lds = large ? kLargeLds : kSmallLds;

@@ -1,0 +1,171 @@
+// switch_linear's forward product for few rows (a decoding step): bound by the one pass over W.
+//
+// W goes from memory to the registers, 16 bytes per lane, and is used by up to four MFMA row blocks of 16 rows of x.  A
+// wave takes chunks of k rows of W (32 of bf16, 16 of fp32) by 16 x 16 bytes of columns: lane 16 g + c holds, of the
+// rows that are lane group g's share of the MFMA's k, chunk c of columns.  Column j of chunk c is index c of MFMA j, so
+// no element changes lanes; bf16 pairs of k come from two registers by a byte permutation.  Eight waves of a block take
+// every eighth chunk of the block's part of k and add up their sums through LDS, in order; several parts of k
+// (few columns) are added up by linear_join's kernel.
+#include "linear.h"
+#include "rows_operands.h"
+
+namespace sw {
+
+constexpr int kFewRows = 64, kFewWaves = 8;
+
+template <typename T> struct FewChunk;   // a lane's share of a chunk: W rows of 16 bytes, MFMA operands
+template <> struct FewChunk<bf16> {
+    static constexpr int kRows = 32, kLoads = 8, kOperands = 8;   // k rows, W loads per lane, MFMA per row block
+    u32x4 w[kLoads];
+    // k rows 8 g + i of chunk k
+    __device__ __forceinline__ static int row(int g, int i) { return 8 * g + i; }
+    template <int MT> __device__ __forceinline__ void products(f32x4 (&acc)[8][MT], const u32x4 (&x)[MT]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            u32x4 f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                f[i] = __builtin_amdgcn_perm(w[2 * i + 1][j / 2], w[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+                acc[j][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f),
+                                                                     __builtin_bit_cast(bf16x8, x[m]), acc[j][m], 0, 0, 0);
+        }
+    }
+};
+template <> struct FewChunk<float> {
+    static constexpr int kRows = 16, kLoads = 4, kOperands = 4;
+    u32x4 w[kLoads];
+    __device__ __forceinline__ static int row(int g, int i) { return 4 * g + i; }
+    // (an MFMA takes one k of each lane group: 4 g + i of all g)
+    template <int MT> __device__ __forceinline__ void products(f32x4 (&acc)[4][MT], const u32x4 (&x)[MT]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+                    acc[j][m] = mfma_f32(__uint_as_float(w[i][j]), __uint_as_float(x[m][i]), acc[j][m]);
+    }
+};
+
+template <typename T, int MT, int ACT>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void linear_few_kernel(LinearArgs a, LinearCut cut) {
+    typedef FewChunk<T> Chunk;
+    constexpr bool GATED = ACT == SW_ACT_GEGLU;
+    constexpr int n = Row16<T>::n, kCols = 16 * n, kPitch = kCols + 4;   // columns of a block; LDS row, in floats
+    extern __shared__ __attribute__((aligned(16))) float red[];          // [waves][16][kPitch]
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int p0 = blockIdx.x * (GATED ? kCols / 2 : kCols);
+    const int split = blockIdx.y;
+    const int k0 = (int)(split * cut.split_k), kend = (int)min(a.Kdim, k0 + cut.split_k), K = (int)a.Kdim;
+    // the lane's columns of W; rows past the last one lie past the descriptor
+    const int col = GATED ? p0 + (c & 7) * n : p0 + c * n;
+    const auto wsrc = __builtin_amdgcn_make_buffer_rsrc((void *)a.P, 0, (int)((uint32_t)K * (uint32_t)a.ldp * sizeof(T)), 0x00020000);
+    const auto xsrc = __builtin_amdgcn_make_buffer_rsrc((void *)a.Q, 0, (int)((uint32_t)a.Qdim * (uint32_t)K * sizeof(T)), 0x00020000);
+    const uint32_t wcol = col < a.Pdim ? (uint32_t)(GATED && c >= 8 ? a.Pdim + col : col) * sizeof(T) : kOobOffset;
+    const uint32_t xrow = (uint32_t)c * (uint32_t)K * sizeof(T);
+    Chunk now, next;
+    u32x4 xnow[MT], xnext[MT];
+    auto load = [&](int k, Chunk &ch, u32x4 (&x)[MT]) {
+#pragma unroll
+        for (int i = 0; i < Chunk::kLoads; ++i) {
+            const uint32_t off = (uint32_t)(k + Chunk::row(g, i)) * (uint32_t)a.ldp * sizeof(T) + wcol;
+            ch.w[i] = __builtin_amdgcn_raw_buffer_load_b128(wsrc, (int)off, 0, 0);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {   // (x past its last k must be zero: W's zeros there do not make up for infinities)
+            const int kx = k + Chunk::row(g, 0);
+            const uint32_t off = kx < K && m * 16 + c < a.Qdim ? xrow + (uint32_t)(m * 16 * K + kx) * sizeof(T) : kOobOffset;
+            x[m] = __builtin_amdgcn_raw_buffer_load_b128(xsrc, (int)off, 0, 0);
+        }
+    };
+    f32x4 acc[n][MT];
+#pragma unroll
+    for (int j = 0; j < n; ++j)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[j][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int kStride = kFewWaves * Chunk::kRows;
+    int k = k0 + wave * Chunk::kRows;
+    if (k < kend) load(k, now, xnow);
+    for (; k < kend; k += kStride) {
+        const bool more = k + kStride < kend;
+        if (more) load(k + kStride, next, xnext);
+        now.template products<MT>(acc, xnow);
+        if (more) {
+            now = next;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) xnow[m] = xnext[m];
+        }
+    }
+    // a lane holds, for row c of a block, columns n (4 g + r) + j in acc[j][block][r]
+    const int tid = threadIdx.x, chunks = GATED ? 8 : 16;
+    const int r = tid / chunks, ch = tid % chunks, p = p0 + ch * n;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+        if (m) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < n; j += 4)
+                *(f32x4 *)(red + (wave * 16 + c) * kPitch + n * (4 * g + i) + j) =
+                    f32x4{acc[j][m][i], acc[j + 1][m][i], acc[j + 2][m][i], acc[j + 3][m][i]};
+        __syncthreads();
+        const int64_t q = m * 16 + r;
+        if (r < 16 && q < a.Qdim && p < a.Pdim) {
+            float v[n] = {}, lin[n] = {};
+#pragma unroll
+            for (int w = 0; w < kFewWaves; ++w) {
+                const float *from = red + (w * 16 + r) * kPitch + ch * n;
+#pragma unroll
+                for (int j = 0; j < n; ++j) {
+                    v[j] += from[j];
+                    if (GATED) lin[j] += from[kCols / 2 + j];
+                }
+            }
+            if (cut.splits > 1) linear_store_part<n, GATED>(a, split, q, p, v, lin);
+            else linear_emit<T, ACT>(a, q, p, v, lin);
+        }
+    }
+}
+
+bool linear_few_rows(const switch_linear_config *cfg) { return cfg->M <= kFewRows; }
+
+// Parts of k that give every CU a block, as long as each wave has two chunks.
+LinearCut linear_few_cut(const switch_linear_config *cfg) {
+    const bool bf = cfg->act_dtype == SW_BF16;
+    const int64_t tiles = ceil_div(linear_columns(cfg), bf ? 128 : 64), least = kFewWaves * (bf ? 32 : 16) * 2;
+    int64_t splits = 256 / tiles;
+    if (splits > cfg->K / least) splits = cfg->K / least;
+    if (splits < 2) return LinearCut{1, cfg->K};
+    const int64_t split_k = ceil_div(ceil_div(cfg->K, splits), 32) * 32;
+    return LinearCut{(int)ceil_div(cfg->K, split_k), split_k};
+}
+
+template <typename T, int ACT> static hipError_t linear_few(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
+    constexpr int n = Row16<T>::n, lds = kFewWaves * 16 * (16 * n + 4) * 4;
+    const int mt = (int)ceil_div(a.Qdim, 16);
+    auto kern = mt == 1 ? linear_few_kernel<T, 1, ACT> : mt == 2 ? linear_few_kernel<T, 2, ACT> : linear_few_kernel<T, 4, ACT>;
+    static PerDeviceOnce once[3];
+    const hipError_t err = with_lds(once[mt == 1 ? 0 : mt == 2 ? 1 : 2], kern, lds);
+    if (err != hipSuccess) return err;
+    const dim3 grid((unsigned)ceil_div(a.Pdim, a.gated ? 8 * n : 16 * n), (unsigned)plan.x.splits);
+    hipLaunchKernelGGL(kern, grid, dim3(64 * kFewWaves), lds, s, a, plan.x);
+    return hipGetLastError();
+}
+
+template <typename T> static hipError_t linear_few_act(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
+    switch (a.act) {
+    case SW_ACT_RELU: return linear_few<T, SW_ACT_RELU>(plan, a, s);
+    case SW_ACT_GELU: return linear_few<T, SW_ACT_GELU>(plan, a, s);
+    case SW_ACT_GEGLU: return linear_few<T, SW_ACT_GEGLU>(plan, a, s);
+    default: return linear_few<T, SW_ACT_NONE>(plan, a, s);
+    }
+}
+
+hipError_t launch_linear_few(int dtype, const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
+    return dtype == SW_BF16 ? linear_few_act<bf16>(plan, a, s) : linear_few_act<float>(plan, a, s);
+}
+
+}  // namespace sw

@@ -67,4 +67,17 @@ template <> struct Eight<float> {
     }
 };
 
+// 16 bytes of consecutive elements as floats.
+template <typename T> struct Row16 {
+    static constexpr int n = 16 / sizeof(T);
+    static __device__ __forceinline__ void load(const void *p, int64_t at, float *v) {
+        if constexpr (n == 8) Eight<T>::load((const T *)p + at, v);
+        else *(float4 *)v = *(const float4 *)((const T *)p + at);
+    }
+    static __device__ __forceinline__ void store(void *p, int64_t at, const float *v) {
+        if constexpr (n == 8) Eight<T>::store((T *)p + at, v);
+        else *(float4 *)((T *)p + at) = *(const float4 *)v;
+    }
+};
+
 }  // namespace sw
