@@ -184,7 +184,7 @@ struct LinearModel {
     int resident;
 };
 static const LinearModel kBf16Models[] = {{256, 64, 1.45, 1.45, 10., 1}, {128, 64, 0.52, 0.75, 8., 2}};
-static const LinearModel kF32Models[] = {{64, 32, 0.45, 0.6, 5., 4}};
+static const LinearModel kF32Models[] = {{64, 32, 0.5, 0.6, 5., 3}};
 constexpr int kCUs = 256;
 constexpr double kJoinUs = 4., kJoinGbs = 4000.;   // of a launch that adds up parts, and its traffic's rate
 

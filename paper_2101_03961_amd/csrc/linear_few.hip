@@ -45,7 +45,8 @@ template <> struct FewChunk<float> {
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
-                    acc[j][m] = mfma_f32(__uint_as_float(w[i][j]), __uint_as_float(x[m][i]), acc[j][m]);
+                    acc[j][m] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i][j]), __uint_as_float(x[m][i]),
+                                                                      acc[j][m], 0, 0, 0);
     }
 };
 

@@ -1,4 +1,4 @@
-// Operand tiles of gemm_rows.hip, gemm_wgrad.hip, gemm_f32.hip, router_block.hip, linear_bf16.hip and linear_f32.hip: R rows by a step's k, filled by
+// Operand tiles of gemm_rows.hip, gemm_wgrad.hip, gemm_f32.hip, router_block.hip and linear_*.hip: R rows by a step's k, filled by
 // NW waves with direct global -> LDS loads.  In a step that the end of k cuts, k past the end reads as zeros; of a
 // step wholly past it, which is loaded to keep the wait counts even and never read, nothing is said (its 32-bit
 // offsets may wrap back into the descriptor).
@@ -90,52 +90,6 @@ template <int R, int NW, int S = 32> struct F32Direct : RowsDirect<R, NW, 64> {
     }
     int part;
 };
-
-// fp32 [k][row] operand of MFMA tiles of S x S: LDS [32 k][R]; rows S apart trade places in odd k-rows (S = 16: in k-rows 4 n + 2 and
-// 4 n + 3), so that the k-rows of a read use different banks.
-template <int R, int NW, int S> struct F32Trans {
-    static_assert(S == 32 ? R > 32 : R == 32, "rows S apart, whose k-rows would meet in a bank");
-    static __device__ __forceinline__ int turn(int k) { return S == 32 ? (k & 1) << 5 : (k >> 1 & 1) << 4; }
-    static constexpr int kLoads = R * 32 * 4 / (1024 * NW);
-    static constexpr int kChunks = R / 4;              // 16-byte chunks of a k-row
-    static constexpr int kRowsPerLoad = 64 / kChunks;  // k-rows of one wave-wide load
-    static_assert(kLoads * NW * kRowsPerLoad == 32 && kRowsPerLoad % (64 / S) == 0, "k-rows divide over the waves");
-    i32x4 rsrc;
-    uint32_t voff, k_step, frag0;
-    __device__ __forceinline__ void init(const float *base, int ld, int row0, int rowlim, int klim,
-                                         int lane, int wave) {
-        rsrc = make_rsrc(base, (uint32_t)klim * (uint32_t)ld * 4u);
-        k_step = (uint32_t)ld * 4u;
-        const int kk = lane / kChunks;
-        const int row = row0 + ((lane % kChunks) ^ (turn(kk) >> 2)) * 4;
-        voff = row < rowlim ? ((uint32_t)(wave * kLoads * kRowsPerLoad + kk) * (uint32_t)ld + (uint32_t)row) * 4u
-                            : kOobOffset;
-    }
-    __device__ __forceinline__ void init_frag(int lane, int frag_row) {
-        const int h = lane / S;
-        frag0 = (uint32_t)((h * R + ((frag_row + lane % S) ^ turn(h))) * 4);
-    }
-    __device__ __forceinline__ void issue_one(uint32_t st, int k0, int wave, int i) const {
-        dma16(rsrc, voff, (uint32_t)(k0 + i * kRowsPerLoad) * k_step,
-              st + (uint32_t)((wave * kLoads + i) * 1024));
-    }
-    // element m: k = 8 ks + 64 / S m + lane / S
-    __device__ __forceinline__ f32x4 frag4(const char *st, int x, int ks) const {
-        const char *p = st + (frag0 ^ (uint32_t)(x << 7)) + ks * (8 * R * 4);
-        f32x4 v = {};
-#pragma unroll
-        for (int m = 0; m < S / 8; ++m) v[m] = *(const float *)(p + m * (64 / S * R * 4));
-        return v;
-    }
-};
-
-// MFMA tiles of S x S, S 32 or 16
-__device__ __forceinline__ f32x16 mfma_f32(float p, float q, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(p, q, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma_f32(float p, float q, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x4f32(p, q, c, 0, 0, 0);
-}
 
 // [k][row] operand of R rows for MFMA 16x16x32: LDS [64 k][R].  One transposing read (ds_read_b64_tr_b16) has lanes
 // 0..31 fetch 32 bytes (16 rows) from each of eight k-rows, 0..3 and 8..11 of the fragment, lanes 32..63 those 16
