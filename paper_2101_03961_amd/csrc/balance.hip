@@ -112,12 +112,23 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+    // (the next row's logits are under way while a row is worked on)
     int seen = 0;
+    auto live = [&](int64_t t) { return t < tend && (!a.mask || a.mask[t]); };
+    float next[NV][4];
+    bool have = live(t0 + sub);
+    if (have) balance_row<G, NV, WIDE>(a.logits + (t0 + sub) * a.E, a.E, lane, next);
     for (int64_t t = t0 + sub; t < tend; t += kRows) {
-        if (a.mask && !a.mask[t]) continue;
-        ++seen;
         float h[NV][4];
-        balance_row<G, NV, WIDE>(a.logits + t * a.E, a.E, lane, h);
+        const bool now = have;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[i][j] = next[i][j];
+        have = live(t + kRows);
+        if (have) balance_row<G, NV, WIDE>(a.logits + (t + kRows) * a.E, a.E, lane, next);
+        if (!now) continue;
+        ++seen;
         balance_probs<G, NV>(h);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -145,6 +156,27 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a) {
         }
         __syncthreads();
     }
+    if (gridDim.x == 1) {   // the only block: no parts to join
+        __shared__ double sums[kBalThreads / kWave];
+        double sum = 0.;
+        for (int i = tid; i < a.E; i += kBalThreads) {
+            a.counts[i] = hist[i];
+            sum += (double)psum[i] * (double)hist[i];
+        }
+#pragma unroll
+        for (int m = kWave / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m, kWave);
+        if (tid % kWave == 0) sums[tid / kWave] = sum;
+        __syncthreads();
+        if (tid == 0) {
+            sum = 0.;
+#pragma unroll
+            for (int w = 0; w < kBalThreads / kWave; ++w) sum += sums[w];
+            const double n = live_tokens > 0 ? (double)live_tokens : 1.;
+            a.tokens[0] = live_tokens;
+            *a.loss = (float)(a.alpha * a.E / a.k * (sum / (n * n)));
+        }
+        return;
+    }
     const size_t at = (size_t)blockIdx.x * a.E;
     for (int i = tid; i < a.E; i += kBalThreads) {
         a.psum_part[at + i] = psum[i];
@@ -167,6 +199,7 @@ __global__ __launch_bounds__(1024) void balance_join_kernel(BalanceArgs a) {
     double p = 0.;
     int32_t c = 0, n = 0;
     if (e < a.E)
+#pragma unroll 8
         for (int b = line; b < a.nbg; b += kLines) {
             p += (double)a.psum_part[(b0 + b) * a.E + e];
             c += a.count_part[(b0 + b) * a.E + e];
@@ -241,6 +274,11 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(BalanceBwdArgs
     const int g = blockIdx.x / a.nbg;
     const int64_t t0 = g * a.Tg + (int64_t)(blockIdx.x - g * a.nbg) * a.tb;
     const int64_t gend = (g + 1) * a.Tg, tend = t0 + a.tb < gend ? t0 + a.tb : gend;
+    // (the first row's logits are under way while the coefficients are made, the next one's while a row is worked on)
+    auto live = [&](int64_t t) { return t < tend && (!a.mask || a.mask[t]); };
+    float next[NV][4];
+    bool have = live(t0 + sub);
+    if (have) balance_row<G, NV, WIDE>(a.logits + (t0 + sub) * a.E, a.E, lane, next);
     const int32_t *counts = a.counts + (size_t)g * a.E;
     int64_t total = 0;
     for (int i = tid; i < a.E; i += kBalThreads) total += counts[i];
@@ -263,13 +301,14 @@ __global__ __launch_bounds__(kBalThreads) void balance_bwd_kernel(BalanceBwdArgs
         }
     for (int64_t t = t0 + sub; t < tend; t += kRows) {
         float h[NV][4];
-        if (a.mask && !a.mask[t]) {
+        const bool now = have;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) h[i][j] = 0.f;
-        } else {
-            balance_row<G, NV, WIDE>(a.logits + t * a.E, a.E, lane, h);
+            for (int j = 0; j < 4; ++j) h[i][j] = now ? next[i][j] : 0.f;
+        have = live(t + kRows);
+        if (have) balance_row<G, NV, WIDE>(a.logits + (t + kRows) * a.E, a.E, lane, next);
+        if (now) {
             balance_probs<G, NV>(h);
             float dot = 0.f;
 #pragma unroll
@@ -338,7 +377,11 @@ static BalanceLayout balance_layout(const switch_balance_config *cfg) {
     BalanceLayout l{};
     l.groups = cfg->n_groups > 1 ? cfg->n_groups : 1;
     l.Tg = cfg->T / l.groups;
-    l.tb = balance_tokens(cfg, 512);
+    // 512 blocks; more experts than 1024: 256, whose parts are half as many bytes (us, 256 / 512 / 1024 blocks: 65536 x 128
+    // 15.6 / 14.9 / 17.8, 65536 x 512 38 / 33 / 36, 16384 x 2048 37 / 39 / 41, 4096 x 4096 25 / 28 / 37).  Four rounds of rows
+    // or fewer: one block, without the second launch (9 us for both, however little they do).
+    l.tb = balance_tokens(cfg, cfg->E > 1024 ? 256 : 512);
+    if (l.groups == 1 && cfg->T <= 4 * balance_rows(cfg->E)) l.tb = 4 * balance_rows(cfg->E);
     l.nbg = ceil_div(l.Tg, l.tb);
     l.tiles = ceil_div(cfg->E, kBalJoinCols);
     size_t off = 0;
@@ -427,6 +470,7 @@ int switch_balance_loss(const switch_balance_config *cfg, const float *logits, c
 #undef SW_BALANCE
         if ((st = status_of(hipGetLastError()))) return st;
     }
+    if (l.groups * l.nbg == 1) return SW_OK;
     ProfScope ps("balance_join", s);
     hipLaunchKernelGGL(balance_join_kernel, dim3((unsigned)l.tiles, (unsigned)l.groups), dim3(1024), 0, s, a);
     return status_of(hipGetLastError());
@@ -452,7 +496,9 @@ int switch_balance_loss_backward(const switch_balance_config *cfg, float d_loss,
     a.dlogits = dlogits;
     a.Tg = cfg->T / groups;
     a.E = (int)cfg->E;
-    a.tb = (int)balance_tokens(cfg, 1024);
+    // (us, 512 / 1024 / 2048 blocks: 65536 x 32 7.3 / 6.7 / 6.9, 65536 x 128 13.8 / 13.9 / 17.7, 16384 x 2048 55 / 57 / 63,
+    // 4096 x 4096 35 / 48 / 48)
+    a.tb = (int)balance_tokens(cfg, 512);
     a.nbg = (int)ceil_div(a.Tg, a.tb);
     a.scale = (double)d_loss * cfg->alpha * cfg->E / ((double)groups * cfg->k);
     ProfScope ps("balance_bwd", s);
