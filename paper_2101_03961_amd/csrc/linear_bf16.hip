@@ -50,17 +50,24 @@ __device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const Linea
     const bool in = p < a.Pdim;
     LinearColumns<bf16, ACT> col;
     if (KIND == LINEAR_FWD && in) col.load(a, p);
+    // the residual's rows, kAhead rounds before they are added (the fragments' registers are free by now)
+    constexpr int kAhead = 4;
+    bf16x8 res[2 * IQ][kPasses];
+    auto load_residual = [&](int j) {
+#pragma unroll
+        for (int x = 0; x < kPasses; ++x) {
+            const int row = j * 16 + x * kPassRows + r0;
+            if (row < rows && in) res[j][x] = *(const bf16x8 *)((const bf16 *)a.residual + (q0 + row) * a.Pdim + p);
+        }
+    };
+    if (KIND == LINEAR_FWD && a.residual)
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (j < 2 * IQ) load_residual(j);
 #pragma unroll
     for (int j = 0; j < 2 * IQ; ++j) {
         if (j * 16 >= rows) break;
-        bf16x8 res[kPasses];
-        if (KIND == LINEAR_FWD && a.residual) {
-#pragma unroll
-            for (int x = 0; x < kPasses; ++x) {
-                const int row = j * 16 + x * kPassRows + r0;
-                if (row < rows && in) res[x] = *(const bf16x8 *)((const bf16 *)a.residual + (q0 + row) * a.Pdim + p);
-            }
-        }
+        if (KIND == LINEAR_FWD && a.residual && j + kAhead < 2 * IQ) load_residual(j + kAhead);
 #pragma unroll
         for (int i = 0; i < 2 * IP; ++i)
             *(f32x4 *)(turn + (lane & 15) * kPitch + (((i * 4 + (lane >> 4)) ^ (lane & 15)) << 4)) = acc[i][j];
@@ -83,7 +90,7 @@ __device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const Linea
                 float r8[8];
                 if (a.residual)
 #pragma unroll
-                    for (int m = 0; m < 8; ++m) r8[m] = (float)res[x][m];
+                    for (int m = 0; m < 8; ++m) r8[m] = (float)res[j][x][m];
                 linear_emit<bf16, ACT>(a, col, q, p, v, lin, r8);
             } else {
 #pragma unroll
