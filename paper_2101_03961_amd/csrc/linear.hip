@@ -177,20 +177,21 @@ template <typename T> static hipError_t linear_finish(const LinearArgs &a, int s
 
 // ---- how a product is cut ---------------------------------------------------------------------
 // Per kind of tile: k of a step; us of a step per block of a CU (of the blocks that share it, one after the other) and of
-// a step at least; us of a block's start and end; blocks that a CU holds.  Measured with products of 4 to 64 steps.
+// a step at least; us of a block's start and end, forward and backward (whose parts of dW are stored in fp32); blocks that a
+// CU holds.  Fitted to products of 4 to 64 steps and to backward passes with 1 to 48 parts of dW; us of dx and dW, as chosen
+// (tile, parts) / the best of all: 16384 x 768 x 2048 (256, 12) 119 / 119; 65536 x 2048 x 768 (256, 8) 461 / 461; 8192 x 2048 x 768
+// (256, 8) 75 / 67; 5000 x 520 x 1000 (128, 6) 27 / 27; 2048 x 4096 x 4096 (256, 1) 119 / 118; 30000 x 264 x 520 (128, 16) 48 / 46.
 struct LinearModel {
     int tile, bk;
-    double step, least, once;
+    double step, least, once_fwd, once_bwd;
     int resident;
 };
-static const LinearModel kBf16Models[] = {{256, 64, 1.45, 1.45, 10., 1}, {128, 64, 0.52, 0.75, 8., 2}};
-static const LinearModel kF32Models[] = {{64, 32, 0.5, 0.6, 5., 3}};
+static const LinearModel kBf16Models[] = {{256, 64, 1.45, 1.45, 10., 17., 1}, {128, 64, 0.52, 0.75, 8., 8., 2}};
+static const LinearModel kF32Models[] = {{64, 32, 0.5, 0.6, 5., 5., 3}};
 constexpr int kCUs = 256;
-constexpr double kJoinUs = 4., kJoinGbs = 4000.;   // of a launch that adds up parts, and its traffic's rate
-
-static double join_us(int splits, double elements) {
-    return splits > 1 ? kJoinUs + splits * elements * 8e-3 / kJoinGbs : 0.;
-}
+// A launch that adds up parts of k: forward, with the epilogue, or backward.
+static double finish_us(int splits, double elements) { return splits > 1 ? 4. + splits * elements * 2e-6 : 0.; }
+static double join_us(int splits, double elements) { return splits > 1 ? 3. + splits * elements * 0.67e-6 : 0.; }
 static LinearCut cut_of(int64_t k, int splits, int bk) {
     const int64_t split_k = ceil_div(ceil_div(k, splits), bk) * bk;
     return LinearCut{(int)ceil_div(k, split_k), split_k};
@@ -216,11 +217,10 @@ LinearPlan plan_linear(const switch_linear_config *cfg, bool backward) {
             if (sx > 1 && (tx * sx > 2 * kCUs || kx < (int64_t)sx * 4 * m.bk)) break;
             const LinearCut x = cut_of(kx, sx, m.bk);
             const double steps_x = (double)ceil_div(x.split_k, m.bk), items_x = tx * x.splits;
-            auto time_of = [&](double per_cu, double steps) {
-                return ceil(per_cu / m.resident) * m.once + steps * fmax(per_cu * m.step, m.least);
-            };
             if (!backward) {
-                const double us = time_of(ceil(items_x / kCUs), steps_x) + join_us(x.splits, (double)M * Nz);
+                const double per_cu = ceil(items_x / kCUs);
+                const double us = ceil(per_cu / m.resident) * m.once_fwd + steps_x * fmax(per_cu * m.step, m.least) +
+                                  finish_us(x.splits, (double)M * Nz);
                 if (us < best) {
                     best = us;
                     plan = LinearPlan{m.tile, x, {1, M}};
@@ -239,7 +239,7 @@ LinearPlan plan_linear(const switch_linear_config *cfg, bool backward) {
                 found = true;
                 const double steps_w = (double)ceil_div(w.split_k, m.bk), items_w = tw * w.splits;
                 // dx's tiles, then dW's on what they leave idle: whole blocks
-                const double bx = steps_x * m.step + m.once / m.resident, bw = steps_w * m.step + m.once / m.resident;
+                const double once = m.once_bwd / m.resident, bx = steps_x * m.step + once, bw = steps_w * m.step + once;
                 const double rounds = floor(items_x / kCUs), over = items_x - rounds * kCUs, t0 = rounds * bx;
                 double end = fmax(t0 + (over > 0 ? bx : 0.), (items_x * bx + items_w * bw) / kCUs);
                 for (int j = 0; j < 16; ++j) {
@@ -248,7 +248,7 @@ LinearPlan plan_linear(const switch_linear_config *cfg, bool backward) {
                     const double a = t0 + bx + (na + 1.) * bw, b = t0 + (nb + 1.) * bw;
                     end = over > 0 && a < b ? a : b;
                 }
-                end = fmax(end, fmax(steps_x, steps_w) * m.least + m.once);
+                end = fmax(end, fmax(steps_x, steps_w) * m.least + m.once_bwd);
                 const double us = end + join_us(x.splits, (double)M * K) + join_us(w.splits, (double)K * Nz);
                 if (us < best) {
                     best = us;
