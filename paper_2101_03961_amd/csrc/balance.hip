@@ -97,6 +97,11 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a) {
     const int g = blockIdx.x / a.nbg;
     const int64_t t0 = g * a.Tg + (int64_t)(blockIdx.x - g * a.nbg) * a.tb;
     const int64_t gend = (g + 1) * a.Tg, tend = t0 + a.tb < gend ? t0 + a.tb : gend;
+    // (the first row's logits are under way while the choices are counted, the next one's while a row is worked on)
+    auto live = [&](int64_t t) { return t < tend && (!a.mask || a.mask[t]); };
+    float next[NV][4];
+    bool have = live(t0 + sub);
+    if (have) balance_row<G, NV, WIDE>(a.logits + (t0 + sub) * a.E, a.E, lane, next);
     if (blockIdx.x == 0 && tid == 0) *a.arrived = 0;   // for the kernel behind this one
     for (int i = tid; i < kCols; i += kBalThreads) hist[i] = 0;
     if (tid == 0) live_tokens = 0;
@@ -112,12 +117,7 @@ __global__ __launch_bounds__(kBalThreads) void balance_kernel(BalanceArgs a) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-    // (the next row's logits are under way while a row is worked on)
     int seen = 0;
-    auto live = [&](int64_t t) { return t < tend && (!a.mask || a.mask[t]); };
-    float next[NV][4];
-    bool have = live(t0 + sub);
-    if (have) balance_row<G, NV, WIDE>(a.logits + (t0 + sub) * a.E, a.E, lane, next);
     for (int64_t t = t0 + sub; t < tend; t += kRows) {
         float h[NV][4];
         const bool now = have;

@@ -186,7 +186,7 @@ struct LinearModel {
     double step, least, once_fwd, once_bwd;
     int resident;
 };
-static const LinearModel kBf16Models[] = {{256, 64, 1.45, 1.45, 10., 17., 1}, {128, 64, 0.52, 0.75, 8., 8., 2}};
+static const LinearModel kBf16Models[] = {{256, 64, 1.45, 1.45, 10., 17., 1}, {128, 64, 0.52, 0.75, 4., 8., 2}};
 static const LinearModel kF32Models[] = {{64, 32, 0.5, 0.6, 5., 5., 3}};
 constexpr int kCUs = 256;
 // A launch that adds up parts of k: forward, with the epilogue, or backward.
@@ -206,6 +206,8 @@ LinearPlan plan_linear(const switch_linear_config *cfg, bool backward) {
     // the rows of a part of dW: what a descriptor of 2 GB spans
     const int64_t widest = (K > Nz ? K : Nz) * (bf ? 2 : 4), most_k = (int64_t)0x7fffffff / widest / 64 * 64;
     static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+    // the normal distribution function of a large tile's values, which no other block's products hide
+    const double gelu_us = cfg->activation == SW_ACT_GELU ? 9. : cfg->activation == SW_ACT_GEGLU ? 5. : 0.;
     double best = 1e30;
     const LinearModel *models = bf ? kBf16Models : kF32Models;
     for (int i = 0; i < (bf ? 2 : 1); ++i) {
@@ -219,8 +221,8 @@ LinearPlan plan_linear(const switch_linear_config *cfg, bool backward) {
             const double steps_x = (double)ceil_div(x.split_k, m.bk), items_x = tx * x.splits;
             if (!backward) {
                 const double per_cu = ceil(items_x / kCUs);
-                const double us = ceil(per_cu / m.resident) * m.once_fwd + steps_x * fmax(per_cu * m.step, m.least) +
-                                  finish_us(x.splits, (double)M * Nz);
+                const double us = ceil(per_cu / m.resident) * (m.once_fwd + (m.resident == 1 ? gelu_us : 0.)) +
+                                  steps_x * fmax(per_cu * m.step, m.least) + finish_us(x.splits, (double)M * Nz);
                 if (us < best) {
                     best = us;
                     plan = LinearPlan{m.tile, x, {1, M}};

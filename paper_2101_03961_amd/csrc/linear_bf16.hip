@@ -1,9 +1,11 @@
-// switch_linear's products on bf16 MFMA, fp32 accumulation.
+// switch_linear's products on bf16 MFMA 16x16x32, fp32 accumulation (P is the MFMA "A" side).  One tile per block, k 64 at a
+// time through LDS stages filled by direct loads.
 //
-// Two kinds of tile.  Large ones, 256 x 256 in eight waves of 64 x 128 (MFMA 16x16x32; P is the "A" side), by persistent
-// blocks, one per CU: the loads run one (Q) and two (P) steps of 64 k ahead of the products, over the end of a tile into the
-// block's next one, so that a tile's first loads and its stores overlap with products.  Small ones, 128 x 128 in four waves, two
-// blocks per CU, for products with too few large tiles.
+// Large tiles, 256 x 256 in four waves, one block per CU, for products that fill the chip with them: bound by the matrix cores
+// under their own power (8192 x 8192 x 8192: 1320 - 1450 TFLOP/s; 8192 x 8192 x 4096 of zeros, which draw less, 1600 - 1780), and by a tile's start
+// and end, 10 us beside 1.45 us a step: at its end all CUs store at once.  (Persistent blocks of eight waves with the next tile's loads under way
+// during the epilogue: 65536 x 2048 x 768 205 us, the plain eight-wave kernel 202.)  Small tiles, 128 x 128, two blocks per CU,
+// where the large ones leave CUs idle.  linear.hip chooses.
 #include "linear.h"
 #include "rows_operands.h"
 

@@ -94,12 +94,16 @@ def close(name, got, want, bound, norm):
 
 
 SIZES = [(1, 64, 128), (1, 8, 8), (3, 768, 2048), (16, 520, 136), (17, 200, 1000), (33, 1024, 264), (64, 264, 64),
-         (65, 136, 520), (129, 72, 392), (255, 1000, 200), (300, 64, 24), (513, 328, 776), (1025, 256, 256)]
+         (65, 136, 520), (129, 72, 392), (255, 1000, 200), (300, 64, 24), (513, 328, 776), (1025, 256, 256),
+         # tiles cut to one chunk; parts of k of y, of dx, of dW; few rows whose last round is cut
+         (200, 8, 8), (70, 8, 264), (130, 264, 8), (128, 4096, 256), (100, 256, 4096), (5000, 64, 72), (33, 4104, 128),
+         (48, 2600, 1000)]
 
 
 @pytest.mark.parametrize("act", ACTS)
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("M,K,N", SIZES)
+@pytest.mark.parametrize("M,K,N,dtype", [s + (t,) for s in SIZES for t in ("bf16", "f32")]
+                         # fp32 rows of single 16-byte chunks
+                         + [(1, 4, 4, "f32"), (65, 4, 12, "f32"), (100, 12, 4, "f32"), (300, 20, 36, "f32")])
 def test_linear_forward_and_backward(M, K, N, dtype, act):
     rate = (0.0, 0.1)[(M + K) % 2 == 0 or act == "none"]
     seed = 0x123456789ABCDEF + M
@@ -108,6 +112,7 @@ def test_linear_forward_and_backward(M, K, N, dtype, act):
     u = U[dtype]
     for t in (op.y, op.dx, op.dW, op.db) + (() if op.z is None else (op.z,)):
         t.fill_(float("nan"))   # everything is written
+    op.workspace.fill_(255)     # and nothing read that is not (bytes of NaN)
     y = op.forward(dev["x"], dev["W"], dev["bias"], dev["residual"])
     grads = op.backward(dev["dy"], dev["x"], dev["W"])
     torch.cuda.synchronize()
@@ -207,6 +212,86 @@ def test_rows_beyond_the_last_stay_as_they_were():
             for k, s in shapes.items():
                 assert (big[k][:32] == 3.0).all() and (big[k][32 + s[0]:] == 3.0).all(), (k, M, dtype)
                 assert not (big[k][32:32 + s[0]] == 3.0).all(), (k, M, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(3, 40, 72), (64, 264, 136), (200, 72, 264), (1030, 520, 264)])
+def test_infinities_stay_in_their_rows_and_columns(M, K, N, dtype):
+    """The rows beside one of infinities, and the columns beside one of W: the same bits as without them (what is read past
+    the end of a row, for whole tiles, must not be multiplied into another)."""
+    _, dev = linear_case(M, K, N, "none", dtype, 31)
+    op = SwitchLinear(M, K, N, "none", 0.0, 0, dtype, DEV, train=True)
+    y = op.forward(dev["x"], dev["W"]).clone()
+    g = {k: v.clone() for k, v in op.backward(dev["dy"], dev["x"], dev["W"]).items()}
+    x, W, dy = dev["x"].clone(), dev["W"].clone(), dev["dy"].clone()
+    r, c = M // 2, N // 3
+    x[r], W[:, c] = float("inf"), float("nan")
+    rows, cols = torch.arange(M, device=DEV) != r, torch.arange(N, device=DEV) != c
+    assert torch.equal(op.forward(x, W)[rows][:, cols], y[rows][:, cols])
+    dy[r] = float("inf")
+    assert torch.equal(op.backward(dy, dev["x"], dev["W"])["dx"][rows], g["dx"][rows])
+    dy = dev["dy"].clone()
+    dy[:, c] = float("nan")
+    out = op.backward(dy, dev["x"], dev["W"])
+    assert torch.equal(out["dW"][:, cols], g["dW"][:, cols]) and torch.equal(out["db"][cols], g["db"][cols])
+
+
+def test_linear_dropout_is_the_dropout_of_its_output():
+    """Through the unit matrix the products are exact: the same mask, scale and rounding as dropout's."""
+    unit = torch.eye(264, dtype=torch.bfloat16, device=DEV)
+    for M in (5, 100, 600):
+        x = normal(torch.Generator().manual_seed(M), M, 264).to(torch.bfloat16).to(DEV)
+        op = SwitchLinear(M, 264, 264, "none", 0.3, 1 << 40 | M, "bf16", DEV, train=True)
+        assert torch.equal(op.forward(x, unit), dropout(x, 0.3, 1 << 40 | M))
+        # the scale is applied to the sums of the backward pass: one rounding, the same value
+        assert torch.equal(op.backward(x, x, unit)["dx"], dropout(x, 0.3, 1 << 40 | M))
+
+
+def test_linear_of_more_than_two_gigabytes():
+    """x, dy, dx and y past 32-bit byte offsets; the rows of dW's sums in parts that a descriptor spans."""
+    M, K, N = 560001, 2048, 64
+    x = torch.empty(M, K, dtype=torch.bfloat16, device=DEV).normal_()
+    dy = torch.empty(M, N, dtype=torch.bfloat16, device=DEV).normal_()
+    W = torch.empty(K, N, dtype=torch.bfloat16, device=DEV).normal_().mul_(K ** -0.5)
+    op = SwitchLinear(M, K, N, "none", 0.0, 0, "bf16", DEV, train=True)
+    y = op.forward(x, W)
+    g = op.backward(dy, x, W)
+    u = U["bf16"]
+    for at in (0, 262143, 524287, M - 300):
+        rows = slice(at, at + 300)
+        close("y", y[rows], x[rows].cpu().double() @ W.cpu().double(), torch.full((1, 1), math.inf, dtype=torch.float64),
+              u + (math.sqrt(K) + 8) * U32)
+        close("dx", g["dx"][rows], dy[rows].cpu().double() @ W.cpu().double().t(), torch.full((1, 1), math.inf, dtype=torch.float64),
+              u + (math.sqrt(N) + 8) * U32)
+    want = torch.zeros(K, N, dtype=torch.float64, device=DEV)
+    for at in range(0, M, 40000):
+        want += x[at:at + 40000].double().t().contiguous() @ dy[at:at + 40000].double()
+    close("dW", g["dW"], want.cpu(), torch.full((1, 1), math.inf, dtype=torch.float64), u + (math.sqrt(M) + 8) * U32)
+    close("db", g["db"], dy.double().sum(0).cpu(), torch.full((1,), math.inf, dtype=torch.float64),
+          # (columns of random sign: their norm is that of the root sum of squares)
+          2 * (math.sqrt(M) + 16) * U32)
+
+
+def test_linear_calls_on_two_streams():
+    """Two calls at once, each with its own workspace and stream: the same bits as one after the other."""
+    _, dev = linear_case(700, 520, 264, "geglu", "bf16", 12)
+    ops = [SwitchLinear(700, 520, 264, "geglu", 0.1, 5 + i, "bf16", DEV, train=True) for i in range(2)]
+
+    def step(op):
+        op.forward(dev["x"], dev["W"], dev["bias"])
+        op.backward(dev["dy"], dev["x"], dev["W"])
+        return [op.y, op.z, op.dx, op.dW, op.db]
+
+    want = [[t.clone() for t in step(op)] for op in ops]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ops]
+    for _ in range(5):
+        for op, s in zip(ops, streams):
+            with torch.cuda.stream(s):
+                step(op)
+    torch.cuda.synchronize()
+    for op, w in zip(ops, want):
+        assert all(torch.equal(a, b) for a, b in zip([op.y, op.z, op.dx, op.dW, op.db], w))
 
 
 @pytest.mark.parametrize("act", ["gelu", "geglu"])
