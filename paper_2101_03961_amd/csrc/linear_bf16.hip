@@ -139,8 +139,10 @@ __device__ __forceinline__ void products4_load(f32x4 &c0, f32x4 &c1, f32x4 &c2, 
 
 // One large tile: four waves of 128 x 128, one per SIMD, whose fragments take a third less LDS traffic than those of eight
 // waves of 64 x 128 (1536 cycles of reads and fills per step, the products take 2048).  P goes through three stages of 32 KB, Q
-// through two: at the middle of step kt, when both stages of kt are read, the loads of Q for step kt + 2 and of P for kt + 3
-// begin to fill them.  The fragments of a half step are read during the products of the half step before.
+// through two.  In the middle of step kt a barrier ends the reads of its stages; Q's is filled with step kt + 2 in the second half
+// of the step, P's with step kt + 3 in the first half of the next one: a load and two reads per eight products throughout
+// (all 16 loads in the second half: dx of 8192 x 8192 x 4096 380 us, 374 so; of zeros 313 and 301).  The fragments of a half
+// step are read during the products of the half step before.
 template <LinearKind KIND, int ACT>
 __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTiles &t, char *lds, int n) {
     constexpr int IP = 4, WP = 2, IQ = 4, WQ = 2;
@@ -155,7 +157,7 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
     typename S::P op;
     typename S::Q oq;
     constexpr int kLoadsP = S::P::kLoads, kLoadsQ = S::Q::kLoads;
-    static_assert(kLoadsP + kLoadsQ == 16, "a load per group of products");
+    static_assert(kLoadsP == 8 && kLoadsQ == 8, "a load per two groups of products");
     op.init_frag16(lane, wp * 32 * IP);
     oq.init_frag16(lane, wq * 32 * IQ);
     linear_init_p<KIND, GATED, bf16>(op, a, at, lane, wave);
@@ -173,14 +175,13 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
     auto issue_p = [&](uint32_t st, int kt, int i) { op.issue_one(lds0 + st, kt * BK, wave, i); };
     auto issue_q = [&](uint32_t st, int kt, int i) { oq.issue_one(lds0 + 3 * kStageP + st, kt * BK, wave, i); };
 #pragma unroll
-    for (int s = 0; s < 3; ++s) {
+    for (int s = 0; s < 2; ++s) {
 #pragma unroll
         for (int i = 0; i < kLoadsP; ++i) issue_p(s * kStageP, s, i);
 #pragma unroll
-        for (int i = 0; i < kLoadsQ; ++i)
-            if (s < 2) issue_q(s * kStageQ, s, i);
+        for (int i = 0; i < kLoadsQ; ++i) issue_q(s * kStageQ, s, i);
     }
-    rows_wait_vmcnt<2 * kLoadsP + kLoadsQ>();
+    rows_wait_vmcnt<kLoadsP + kLoadsQ>();
     __syncthreads();
     bf16x8 fp[2][2 * IP], fq[2][2 * IQ];
     // fragment f of a half step, in the order of use
@@ -196,7 +197,7 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
     uint32_t sp = 0, sq = 0;   // stages of step kt
 #pragma nounroll
     for (int kt = 0; kt < nk; ++kt) {
-        const uint32_t sp1 = sp == 2 * kStageP ? 0 : sp + kStageP, sq1 = sq ^ kStageQ;
+        const uint32_t sp1 = sp == 2 * kStageP ? 0 : sp + kStageP, sp2 = sp1 == 2 * kStageP ? 0 : sp1 + kStageP, sq1 = sq ^ kStageQ;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             op.reload_frag();
@@ -209,26 +210,27 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
             const char *rp = lds + (ks == 0 ? sp : sp1), *rq = lds + 3 * kStageP + (ks == 0 ? sq : sq1);
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
-                // (the last four groups of the first half cover the reads' latency before the barrier)
-                if (ks == 1 || g < 8) read(rp, rq, ks ^ 1, g);
-                if (ks == 0 && g < 8) read(rp, rq, 1, g + 8);
+                // one read per group; in the first half the last five groups cover the reads' latency before the barrier
+#pragma unroll
+                for (int f = 0; f < kGroups; ++f)
+                    if ((ks == 1 ? f : f * 11 / kGroups) == g) read(rp, rq, ks ^ 1, f);
                 __builtin_amdgcn_sched_barrier(0);
                 const int i = g % 2 * 4, j = g / 2;
-                if (ks == 0) {
-                    products4(acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j], fp[0][i], fp[0][i + 1], fp[0][i + 2],
-                              fp[0][i + 3], fq[0][j]);
+                if (g % 2 == 0) {
+                    products4(acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j], fp[ks][i], fp[ks][i + 1], fp[ks][i + 2],
+                              fp[ks][i + 3], fq[ks][j]);
                 } else {
                     i32x4 rsrc;
                     uint32_t voff, soff, at_lds;
-                    if (g < kLoadsQ) {
-                        oq.load_of((kt + 2) * BK, wave, g, rsrc, voff, soff, at_lds);
-                        at_lds += lds0 + 3 * kStageP + sq;
+                    if (ks == 0) {
+                        op.load_of((kt + 2) * BK, wave, g / 2, rsrc, voff, soff, at_lds);
+                        at_lds += lds0 + sp2;
                     } else {
-                        op.load_of((kt + 3) * BK, wave, g - kLoadsQ, rsrc, voff, soff, at_lds);
-                        at_lds += lds0 + sp;
+                        oq.load_of((kt + 2) * BK, wave, g / 2, rsrc, voff, soff, at_lds);
+                        at_lds += lds0 + 3 * kStageP + sq;
                     }
-                    products4_load(acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j], fp[1][i], fp[1][i + 1], fp[1][i + 2],
-                                   fp[1][i + 3], fq[1][j], rsrc, voff, soff, at_lds);
+                    products4_load(acc[i][j], acc[i + 1][j], acc[i + 2][j], acc[i + 3][j], fp[ks][i], fp[ks][i + 1],
+                                   fp[ks][i + 2], fp[ks][i + 3], fq[ks][j], rsrc, voff, soff, at_lds);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
