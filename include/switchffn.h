@@ -289,7 +289,8 @@ int switch_linear(const switch_linear_config *cfg,
  * be NULL, not all.  z: from switch_linear with the same cfg; not read (may be NULL) for
  * SW_ACT_NONE.  W is read only for dx, x only for dW; the other may be NULL.  With SW_BF16, SW_ACT_GELU
  * and SW_ACT_GEGLU round dz to bf16 for the two products (db sums it in fp32); the others need no
- * rounding: the dropout scale is applied to the sums.  M = 0: dW and db are zeros.
+ * rounding: the dropout scale is applied to the sums.  No output may overlap an input.  M = 0: dW
+ * and db are zeros.
  */
 int switch_linear_backward(const switch_linear_config *cfg,
                            const void *dy,   /* [M, N] act_dtype                       */

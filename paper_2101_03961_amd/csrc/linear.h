@@ -65,10 +65,23 @@ struct LinearTiles {
 static inline LinearTiles linear_tiles(const LinearArgs &a, int tile, const LinearCut &cut) {
     return LinearTiles{(int)ceil_div(a.Qdim, tile), (int)ceil_div(a.Pdim, a.gated ? tile / 2 : tile), cut};
 }
-static inline int64_t linear_items(const LinearTiles &t) { return (int64_t)t.tiles_q * t.tiles_p * t.cut.splits; }
+// blocks of a product, whole rounds of XCDs
+static inline int64_t linear_blocks(const LinearTiles &t) {
+    return ceil_div((int64_t)t.tiles_q * t.tiles_p * t.cut.splits, 8) * 8;
+}
 
-// Item of a block when the blocks of an XCD (b mod 8) take neighbouring ones.
-__device__ __forceinline__ int linear_item(int b, int total) { return (b & 7) * ((total + 7) >> 3) + (b >> 3); }
+// Blocks in two dimensions where one would hold 2^32 threads (whole rounds of XCDs each), and a block's number.
+static inline dim3 linear_grid(int64_t blocks) {
+    const int64_t most = kMaxGridThreads / 256 / 8 * 8, x = blocks < most ? blocks : most;
+    return dim3((unsigned)x, (unsigned)ceil_div(blocks, x));
+}
+__device__ __forceinline__ int linear_block() { return (int)(blockIdx.y * gridDim.x + blockIdx.x); }
+
+// Item of a block when the blocks of an XCD (b mod 8) take neighbouring ones; total or more for blocks without one.
+__device__ __forceinline__ int linear_item(int b, int total) {
+    const int per = (total + 7) >> 3;
+    return b >> 3 < per ? (b & 7) * per + (b >> 3) : total;
+}
 
 // An item's place.  Items of a part of k are neighbours, in bands of eight row tiles, so that those that run on
 // an XCD at a time, 32 in a row, share their operands in its L2.

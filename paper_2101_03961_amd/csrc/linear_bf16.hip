@@ -251,18 +251,18 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
 template <int ACT>
 __global__ __launch_bounds__(256, 1) void linear_fwd_large_kernel(LinearArgs a, LinearTiles t) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(blockIdx.x, total);
+    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(linear_block(), total);
     if (n < total) linear_large<LINEAR_FWD, ACT>(a, t, lds, n);
 }
 
 __global__ __launch_bounds__(256, 1) void linear_bwd_large_kernel(LinearArgs dx, LinearTiles tx, LinearArgs dW, LinearTiles tw,
                                                                   int dx_blocks) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    if ((int)blockIdx.x < dx_blocks) {
-        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(blockIdx.x, total);
+    if (linear_block() < dx_blocks) {
+        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(linear_block(), total);
         if (n < total) linear_large<LINEAR_DX, SW_ACT_NONE>(dx, tx, lds, n);
     } else {
-        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(blockIdx.x - dx_blocks, total);
+        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(linear_block() - dx_blocks, total);
         if (n < total) linear_large<LINEAR_DW, SW_ACT_NONE>(dW, tw, lds, n);
     }
 }
@@ -324,18 +324,18 @@ __device__ __forceinline__ void linear_small(const LinearArgs &a, const LinearTi
 template <int ACT>
 __global__ __launch_bounds__(256, 2) void linear_fwd_small_kernel(LinearArgs a, LinearTiles t) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(blockIdx.x, total);
+    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(linear_block(), total);
     if (n < total) linear_small<LINEAR_FWD, ACT>(a, t, lds, n);
 }
 
 __global__ __launch_bounds__(256, 2) void linear_bwd_small_kernel(LinearArgs dx, LinearTiles tx, LinearArgs dW, LinearTiles tw,
                                                                   int dx_blocks) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    if ((int)blockIdx.x < dx_blocks) {
-        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(blockIdx.x, total);
+    if (linear_block() < dx_blocks) {
+        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(linear_block(), total);
         if (n < total) linear_small<LINEAR_DX, SW_ACT_NONE>(dx, tx, lds, n);
     } else {
-        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(blockIdx.x - dx_blocks, total);
+        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(linear_block() - dx_blocks, total);
         if (n < total) linear_small<LINEAR_DW, SW_ACT_NONE>(dW, tw, lds, n);
     }
 }
@@ -353,7 +353,7 @@ template <int ACT> static hipError_t linear_fwd_bf16(const LinearPlan &plan, con
     const int lds = large ? kLargeLds : kSmallLds;
     const hipError_t err = with_lds(once[large], kern, lds);
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(linear_items(t), 8) * 8)), dim3(256), lds, s, a, t);
+    hipLaunchKernelGGL(kern, linear_grid(linear_blocks(t)), dim3(256), lds, s, a, t);
     return hipGetLastError();
 }
 
@@ -371,13 +371,13 @@ hipError_t launch_linear_backward_bf16(const LinearPlan &plan, const LinearArgs 
     const LinearArgs none{};
     const LinearArgs &ax = dx ? *dx : none, &aw = dW ? *dW : none;
     const LinearTiles tx = linear_tiles(ax, plan.tile, plan.x), tw = linear_tiles(aw, plan.tile, plan.w);
-    const int64_t bx = ceil_div(linear_items(tx), 8) * 8, bw = ceil_div(linear_items(tw), 8) * 8;
+    const int64_t bx = linear_blocks(tx), bw = linear_blocks(tw);
     auto kern = large ? linear_bwd_large_kernel : linear_bwd_small_kernel;
     static PerDeviceOnce once[2];
     const int lds = large ? kLargeLds : kSmallLds;
     const hipError_t err = with_lds(once[large], kern, lds);
     if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(bx + bw)), dim3(256), lds, s, ax, tx, aw, tw, (int)bx);
+    hipLaunchKernelGGL(kern, linear_grid(bx + bw), dim3(256), lds, s, ax, tx, aw, tw, (int)bx);
     return hipGetLastError();
 }
 

@@ -152,25 +152,25 @@ __device__ __forceinline__ void linear_f32_tile(const LinearArgs &a, const Linea
 
 template <int ACT> __global__ __launch_bounds__(256, 3) void linear_fwd_f32_kernel(LinearArgs a, LinearTiles t) {
     __shared__ __attribute__((aligned(16))) char lds[kLds];
-    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(blockIdx.x, total);
+    const int total = t.tiles_q * t.tiles_p * t.cut.splits, n = linear_item(linear_block(), total);
     if (n < total) linear_f32_tile<LINEAR_FWD, ACT>(a, t, lds, n);
 }
 
 __global__ __launch_bounds__(256, 3) void linear_bwd_f32_kernel(LinearArgs dx, LinearTiles tx, LinearArgs dW, LinearTiles tw,
                                                                 int dx_blocks) {
     __shared__ __attribute__((aligned(16))) char lds[kLds];
-    if ((int)blockIdx.x < dx_blocks) {
-        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(blockIdx.x, total);
+    if (linear_block() < dx_blocks) {
+        const int total = tx.tiles_q * tx.tiles_p * tx.cut.splits, n = linear_item(linear_block(), total);
         if (n < total) linear_f32_tile<LINEAR_DX, SW_ACT_NONE>(dx, tx, lds, n);
     } else {
-        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(blockIdx.x - dx_blocks, total);
+        const int total = tw.tiles_q * tw.tiles_p * tw.cut.splits, n = linear_item(linear_block() - dx_blocks, total);
         if (n < total) linear_f32_tile<LINEAR_DW, SW_ACT_NONE>(dW, tw, lds, n);
     }
 }
 
 hipError_t launch_linear_f32(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
     const LinearTiles t = linear_tiles(a, kTile, plan.x);
-    const dim3 grid((unsigned)(ceil_div(linear_items(t), 8) * 8));
+    const dim3 grid = linear_grid(linear_blocks(t));
     auto kern = a.act == SW_ACT_RELU    ? linear_fwd_f32_kernel<SW_ACT_RELU>
                 : a.act == SW_ACT_GELU  ? linear_fwd_f32_kernel<SW_ACT_GELU>
                 : a.act == SW_ACT_GEGLU ? linear_fwd_f32_kernel<SW_ACT_GEGLU>
@@ -183,8 +183,8 @@ hipError_t launch_linear_backward_f32(const LinearPlan &plan, const LinearArgs *
     const LinearArgs none{};
     const LinearArgs &ax = dx ? *dx : none, &aw = dW ? *dW : none;
     const LinearTiles tx = linear_tiles(ax, kTile, plan.x), tw = linear_tiles(aw, kTile, plan.w);
-    const int64_t bx = ceil_div(linear_items(tx), 8) * 8, bw = ceil_div(linear_items(tw), 8) * 8;
-    hipLaunchKernelGGL(linear_bwd_f32_kernel, dim3((unsigned)(bx + bw)), dim3(256), 0, s, ax, tx, aw, tw, (int)bx);
+    const int64_t bx = linear_blocks(tx), bw = linear_blocks(tw);
+    hipLaunchKernelGGL(linear_bwd_f32_kernel, linear_grid(bx + bw), dim3(256), 0, s, ax, tx, aw, tw, (int)bx);
     return hipGetLastError();
 }
 

@@ -111,6 +111,12 @@ def _check(device, want) -> None:
                              % (name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
 
 
+def _device(device) -> torch.device:
+    """The device with its number, as tensors carry it."""
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if device == torch.device("cuda") else device
+
+
 class SwitchLinear:
     """y = residual + dropout(act(x W + bias)) and its gradients (switch_linear).
 
@@ -127,7 +133,7 @@ class SwitchLinear:
         self.cfg = B.SwitchLinearConfig(M, K, N, B.SW_BF16 if dtype == "bf16" else B.SW_F32,
                                         self.ACTIVATIONS[activation], float(dropout), 0, int(seed))
         self.columns = N * (2 if activation == "geglu" else 1)   # of W
-        self.device = torch.device(device)
+        self.device = _device(device)
         self.act = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.workspace_bytes = B.switch_linear_workspace_size(self.cfg, False)
         if train:
@@ -198,7 +204,7 @@ class SwitchBalanceLoss:
         if not torch.cuda.is_available():
             raise RuntimeError("SwitchBalanceLoss needs a GPU: the loss is computed only in the HIP library")
         self.cfg = B.SwitchBalanceConfig(T, E, k, int(n_groups), float(alpha), 0)
-        self.device = torch.device(device)
+        self.device = _device(device)
         self.workspace_bytes = B.switch_balance_workspace_size(self.cfg)
         dev, groups = self.device, max(int(n_groups), 1)
         self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=dev)

@@ -272,6 +272,35 @@ def test_linear_of_more_than_two_gigabytes():
           2 * (math.sqrt(M) + 16) * U32)
 
 
+def test_linear_of_more_tiles_than_one_grid_dimension_holds():
+    """2^30 rows are 2^24 tiles of 256 threads: the blocks take two dimensions, and none of them twice (y is the residual)."""
+    M = (1 << 30) + 77
+    x = torch.empty(M, 4, device=DEV).normal_()
+    y = torch.ones(M, 4, device=DEV)
+    W = torch.empty(4, 4, device=DEV).normal_()
+    cfg = sw.SwitchLinearConfig(M, 4, 4, sw.SW_F32, sw.SW_ACT_NONE, 0.0, 0, 0)
+    assert sw.switch_linear_workspace_size(cfg, False) == 0
+    sw.switch_linear(cfg, x, W, None, y, y, None, None, 0)
+    W64 = W.cpu().double()
+    for at in (0, (1 << 24) - 50, (1 << 29) - 50, (1 << 30) - 100, M - 100):
+        a = x[at:at + 100].cpu().double()
+        want = 1.0 + a @ W64
+        err = (y[at:at + 100].cpu().double() - want).abs()
+        assert (err <= 8 * U32 * (1.0 + a.abs() @ W64.abs())).all(), at
+    # every row: the sums over all of them (fp32 rows, each off by 8 2^-24 of its magnitude, about 4)
+    total = (1.0 * M + x.double().sum(0).cpu() @ W64)
+    assert ((y.double().sum(0).cpu() - total).abs() <= 32 * U32 * 4 * M).all()
+    size = sw.switch_linear_workspace_size(cfg, True)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    dx = torch.full_like(x, float("nan"))
+    sw.switch_linear_backward(cfg, y, None, W, None, dx, None, None, ws, size)
+    for at in (0, (1 << 29) - 50, (1 << 30) - 100, M - 100):
+        a = y[at:at + 100].cpu().double()
+        err = (dx[at:at + 100].cpu().double() - a @ W64.t()).abs()
+        assert (err <= 8 * U32 * (a.abs() @ W64.t().abs())).all(), at
+    assert torch.isfinite(dx.sum(0)).all()
+
+
 def test_linear_calls_on_two_streams():
     """Two calls at once, each with its own workspace and stream: the same bits as one after the other."""
     _, dev = linear_case(700, 520, 264, "geglu", "bf16", 12)
