@@ -123,7 +123,9 @@ def _load():
 
 def _p(t) -> Optional[int]:
     """Device (or host) address of a tensor-like (anything with data_ptr()), an int, or None."""
-    if t is None or type(t) is int:
+    if t is None:
+        return None
+    if isinstance(t, int):
         return t
     return t.data_ptr()
 

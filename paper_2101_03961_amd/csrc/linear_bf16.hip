@@ -4,7 +4,8 @@
 // Large tiles, 256 x 256 in four waves, one block per CU, for products that fill the chip with them: bound by the matrix cores
 // under their own power (8192 x 8192 x 8192: 1320 - 1450 TFLOP/s; 8192 x 8192 x 4096 of zeros, which draw less, 1600 - 1780), and by a tile's start
 // and end, 10 us beside 1.45 us a step: at its end all CUs store at once.  (Persistent blocks of eight waves with the next tile's loads under way
-// during the epilogue: 65536 x 2048 x 768 205 us, the plain eight-wave kernel 202.)  Small tiles, 128 x 128, two blocks per CU,
+// during the epilogue: 65536 x 2048 x 768 205 us, the plain eight-wave kernel 202.  Tiles of 256 x 128, two blocks per CU, whose starts
+// and ends the other block covers, with 32 k a step to fit the LDS: 1.9 us for the products that take 1.45.)  Small tiles, 128 x 128, two blocks per CU,
 // where the large ones leave CUs idle.  linear.hip chooses.
 #include "linear.h"
 #include "rows_operands.h"
