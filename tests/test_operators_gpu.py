@@ -395,6 +395,30 @@ def test_dropout_past_32_bits():
         assert torch.equal(x[first:first + 100].cpu().double(), want), first
 
 
+def test_wrappers_refuse_what_the_kernels_would_misread():
+    x = torch.zeros(8, 16, device=DEV)
+    for bad in (x[:, ::2], x.half(), x.cpu()):
+        with pytest.raises(ValueError):
+            dropout(bad, 0.1, 1)
+    for kw in (dict(residual=x[:4]), dict(residual=x.bfloat16()), dict(out=x.t()), dict(out=x.cpu())):
+        with pytest.raises(ValueError):
+            dropout(x, 0.1, 1, **kw)
+    with pytest.raises(sw.SwitchError):
+        dropout(x, 1.0, 1)
+    with pytest.raises(sw.SwitchError):
+        dropout(x.reshape(-1)[1:], 0.1, 1)   # not on 16 bytes
+    op = SwitchBalanceLoss(8, 16, 2, 0.1, 1, "cuda")
+    index = torch.zeros(8, 2, dtype=torch.int32, device=DEV)
+    mask = torch.ones(8, dtype=torch.uint8, device=DEV)
+    op.forward(x, index, mask)
+    for args in ((x.double(), index, mask), (x[:, :8], index, mask), (x, index.long(), mask), (x, index[:, :1], mask),
+                 (x, index[:, 0], mask), (x, index, mask.bool()), (x, index, mask[:4])):
+        with pytest.raises(ValueError):
+            op.forward(*args)
+    with pytest.raises(ValueError):
+        op.backward(x, mask.float())
+
+
 def balance64(logits, index, mask, groups, alpha, d_loss=1.0):
     T, E = logits.shape
     valid = torch.ones(T, dtype=torch.bool) if mask is None else mask != 0
