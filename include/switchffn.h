@@ -338,7 +338,7 @@ int switch_balance_workspace_size(const switch_balance_config *cfg, size_t *byte
 int switch_balance_loss(const switch_balance_config *cfg,
                         const float *logits,          /* [T, E]                            */
                         const int32_t *expert_index,  /* [T, k]                            */
-                        const uint8_t *token_mask,    /* [T] or NULL                       */
+                        const uint8_t *token_mask,    /* [T] or NULL, on any byte          */
                         float *loss,                  /* [1] (out)                         */
                         int32_t *expert_counts,       /* [n_groups, E] (out)               */
                         int32_t *token_counts,        /* [n_groups] (out) n of each group  */
