@@ -288,8 +288,9 @@ int switch_linear(const switch_linear_config *cfg,
  * db = sum of dz's rows (ReLU'(0) = 0); the residual's gradient is dy itself.  Each of dx, dW, db may
  * be NULL, not all.  z: from switch_linear with the same cfg; not read (may be NULL) for
  * SW_ACT_NONE.  W is read only for dx, x only for dW; the other may be NULL.  With SW_BF16, SW_ACT_GELU
- * and SW_ACT_GEGLU round dz to bf16 for the two products (db sums it in fp32); the others need no
- * rounding: the dropout scale is applied to the sums.  No output may overlap an input.  M = 0: dW
+ * and SW_ACT_GEGLU round dz for the two products (db sums it in fp32): to bf16, or, up to 256 rows, to
+ * the sum of two bf16 terms (an infinite weight may then give NaN in its column of dx); the others need
+ * no rounding: the dropout scale is applied to the sums.  No output may overlap an input.  M = 0: dW
  * and db are zeros.
  */
 int switch_linear_backward(const switch_linear_config *cfg,

@@ -21,7 +21,8 @@ struct LinearArgs {
     const float *bias;
     const void *residual;
     void *C, *z;
-    float *part;                   // k in several parts: their sums, [part][Qdim][columns: of W where gated]
+    float *part;                   // k in several parts: their sums, [part][Qdim][columns: of W where gated]; otherwise nullptr
+                                   // (or dx of dz in two terms: the sums of both)
     int act, gated;
     float scale;                   // of the sums
     Drop drop;

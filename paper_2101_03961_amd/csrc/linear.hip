@@ -13,15 +13,38 @@ namespace sw {
 // dz without the dropout's scale (so that, where act' is 0 or 1, it is dy or zero and loses nothing in bf16) and sums of its
 // rows.  A lane takes a chunk of columns, 16 bytes, of the gate and of the linear part; `lanes` lanes of a block share a row
 // and each handles kDzSteps rows, 256 / lanes apart.  Bound by its traffic.
-constexpr int kDzSteps = 8;
+//
+// GELU's dz has more digits than bf16.  Its rounding adds as much error to a gradient as the gradient's own (together sqrt(2)
+// of one) where many values average it; over few rows a gradient hangs on few of them, and the two came to 1.5 to 2.1 of one
+// (1 to 5 rows; at most 1.55 at 32, 1.48 at 128, 1.47 at 256 and 512).  So up to kTermRows rows dz is kept as the
+// sum of two bf16 terms, 16 digits, the second M rows below the first; the products, which W and dW bind there and not
+// their operations, take 2 M rows: dx's of both terms are added up as parts of k are, dW's k runs over both terms, over x
+// twice.  One term / two, us, 4096 -> 2 x 10240 gated: 16 rows 113 / 116, 256 rows 169 / 196, 1024 rows (were they to have two)
+// 315 / 554; 768 -> 2 x 2048: 1 row 12.5 / 14.0, 256 rows 29 / 35.
+constexpr int kDzSteps = 8, kTermRows = 256, kCopyBlocks = 512;
+static int linear_terms(const switch_linear_config *cfg) {
+    const bool gelu = cfg->activation == SW_ACT_GELU || cfg->activation == SW_ACT_GEGLU;
+    return cfg->act_dtype == SW_BF16 && gelu && cfg->M <= kTermRows ? 2 : 1;
+}
 struct DzArgs {
     const void *dy, *z;
     void *dz;                      // or nullptr
+    int64_t low;                   // where dz's second term begins; 0: one term
+    const void *x;                 // with two terms, copied twice by the blocks behind y_blocks
+    void *x_twice;                 // or nullptr
+    int64_t x_elements;
+    int y_blocks;
     float *part;                   // [row blocks][columns of W], or nullptr
     int64_t M;
     int N, act, lanes;
     Drop drop;
 };
+
+// what a value's rounding to bf16 leaves (exact); nothing where that is infinite
+__device__ __forceinline__ float rest_of(float v) {
+    const float first = (float)(bf16)v;
+    return isfinite(first) ? v - first : 0.f;
+}
 
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
@@ -29,6 +52,20 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
     constexpr int n = C::n, NP = GATED ? 2 : 1;
     __shared__ float sums[256][NP * n + 1];
     const int tid = threadIdx.x, line = tid / a.lanes, lines = 256 / a.lanes;
+    if (sizeof(T) == 2 && (int)blockIdx.y >= a.y_blocks) {
+        const int64_t block = (int64_t)(blockIdx.y - a.y_blocks) * gridDim.x + blockIdx.x;
+        const int64_t step = (int64_t)(gridDim.y - a.y_blocks) * gridDim.x * 256 * n;
+        for (int64_t at = (block * 256 + tid) * n; at < a.x_elements; at += step) {
+            float v[n];
+            C::load(a.x, at, v);
+            C::store(a.x_twice, at, v);
+            // (an infinity counts once: its products with the second terms have either sign)
+#pragma unroll
+            for (int m = 0; m < n; ++m) v[m] = isfinite(v[m]) ? v[m] : 0.f;
+            C::store(a.x_twice, a.x_elements + at, v);
+        }
+        return;
+    }
     const int p = (blockIdx.y * a.lanes + tid % a.lanes) * n;
     const int64_t q0 = (int64_t)blockIdx.x * (lines * kDzSteps) + line;
     const int64_t Nz = NP * (int64_t)a.N;
@@ -62,6 +99,17 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
             if (a.dz) {
                 C::store(a.dz, zat, g);
                 if (GATED) C::store(a.dz, zat + a.N, v);
+                if (sizeof(T) == 2 && a.low) {
+                    float rest[n];
+#pragma unroll
+                    for (int m = 0; m < n; ++m) rest[m] = rest_of(g[m]);
+                    C::store(a.dz, a.low + zat, rest);
+                    if (GATED) {
+#pragma unroll
+                        for (int m = 0; m < n; ++m) rest[m] = rest_of(v[m]);
+                        C::store(a.dz, a.low + zat + a.N, rest);
+                    }
+                }
             }
 #pragma unroll
             for (int m = 0; m < n; ++m) {
@@ -198,7 +246,7 @@ static LinearCut cut_of(int64_t k, int splits, int bk) {
 }
 
 LinearPlan plan_linear(const switch_linear_config *cfg, bool backward) {
-    const int64_t M = cfg->M, K = cfg->K, Nz = linear_columns(cfg);
+    const int64_t M = cfg->M * (backward ? linear_terms(cfg) : 1), K = cfg->K, Nz = linear_columns(cfg);
     LinearPlan plan{64, {1, backward ? Nz : K}, {1, M}};
     if (M == 0) return plan;
     if (!backward && linear_few_rows(cfg)) return LinearPlan{0, linear_few_cut(cfg), {1, M}};
@@ -278,8 +326,10 @@ static int check_linear(const switch_linear_config *cfg) {
 }
 
 struct LinearLayout {
-    size_t dz, db_part, x_part, w_part, total;
+    size_t dz, x_twice, db_part, x_part, w_part, total;
     bool own_dz;                   // dz is not dy itself
+    int terms;                     // of dz
+    int x_parts;                   // sums of y or dx: parts of k, each of every term
     int lanes;                     // of linear_dz_kernel
     int64_t db_parts;
     LinearPlan plan;
@@ -296,11 +346,16 @@ static LinearLayout linear_layout(const switch_linear_config *cfg, bool backward
         l.lanes = 1;
         while (l.lanes < 32 && l.lanes < chunks) l.lanes *= 2;
         l.db_parts = ceil_div(cfg->M, 256 / l.lanes * kDzSteps);
-        l.dz = take(l.own_dz ? (size_t)cfg->M * cols * elt : 0);
+        l.terms = linear_terms(cfg);
+        l.dz = take(l.own_dz ? (size_t)l.terms * cfg->M * cols * elt : 0);
+        l.x_twice = take(l.terms > 1 ? (size_t)2 * cfg->M * cfg->K * elt : 0);
         l.db_part = take((size_t)l.db_parts * cols * 4);
         l.w_part = take(l.plan.w.splits > 1 ? (size_t)l.plan.w.splits * cfg->K * cols * 4 : 0);
+    } else {
+        l.terms = 1;
     }
-    l.x_part = take(l.plan.x.splits > 1 ? (size_t)l.plan.x.splits * cfg->M * (backward ? cfg->K : cols) * 4 : 0);
+    l.x_parts = l.plan.x.splits * l.terms;
+    l.x_part = take(l.x_parts > 1 ? (size_t)l.x_parts * cfg->M * (backward ? cfg->K : cols) * 4 : 0);
     l.total = cfg->M ? off : 0;
     return l;
 }
@@ -339,7 +394,7 @@ int switch_linear(const switch_linear_config *cfg, const void *x, const void *W,
     a.P = W; a.ldp = (int)linear_columns(cfg);
     a.Qdim = cfg->M; a.Kdim = cfg->K; a.Pdim = (int)cfg->N;
     a.bias = bias; a.residual = residual; a.C = y; a.z = z;
-    a.part = (float *)((char *)workspace + l.x_part);
+    a.part = l.x_parts > 1 ? (float *)((char *)workspace + l.x_part) : nullptr;
     a.act = cfg->activation;
     a.gated = cfg->activation == SW_ACT_GEGLU;
     a.scale = 1.f;
@@ -384,7 +439,15 @@ int switch_linear_backward(const switch_linear_config *cfg, const void *dy, cons
         a.part = db ? (float *)(ws + l.db_part) : nullptr;
         a.M = cfg->M; a.N = (int)cfg->N; a.act = cfg->activation; a.lanes = l.lanes;
         a.drop = drop;
-        const dim3 grid((unsigned)l.db_parts, (unsigned)ceil_div(cfg->N, l.lanes * (bf ? 8 : 4)));
+        a.y_blocks = (int)ceil_div(cfg->N, l.lanes * (bf ? 8 : 4));
+        dim3 grid((unsigned)l.db_parts, (unsigned)a.y_blocks);
+        if (l.terms > 1 && (dx || dW)) a.low = cfg->M * cols;
+        if (l.terms > 1 && dW) {
+            a.x = x; a.x_twice = ws + l.x_twice;
+            a.x_elements = cfg->M * cfg->K;
+            const int64_t blocks = ceil_div(a.x_elements, 256 * 8);
+            grid.y += (unsigned)ceil_div(blocks < kCopyBlocks ? blocks : kCopyBlocks, l.db_parts);
+        }
 #define SW_DZ(T, G) hipLaunchKernelGGL((linear_dz_kernel<T, G>), grid, dim3(256), 0, s, a)
         if (bf) { if (gated) SW_DZ(bf16, true); else SW_DZ(bf16, false); }
         else { if (gated) SW_DZ(float, true); else SW_DZ(float, false); }
@@ -395,24 +458,24 @@ int switch_linear_backward(const switch_linear_config *cfg, const void *dy, cons
     ax.scale = aw.scale = drop.scale;
     ax.Q = dz; ax.ldq = (int)cols;
     ax.P = W; ax.ldp = (int)cols;
-    ax.Qdim = cfg->M; ax.Kdim = cols; ax.Pdim = (int)cfg->K;
-    ax.C = dx; ax.part = (float *)(ws + l.x_part);
-    aw.Q = x; aw.ldq = (int)cfg->K;
+    ax.Qdim = l.terms * cfg->M; ax.Kdim = cols; ax.Pdim = (int)cfg->K;
+    ax.C = dx; ax.part = l.x_parts > 1 ? (float *)(ws + l.x_part) : nullptr;
+    aw.Q = l.terms > 1 ? ws + l.x_twice : x; aw.ldq = (int)cfg->K;
     aw.P = dz; aw.ldp = (int)cols;
-    aw.Qdim = cfg->K; aw.Kdim = cfg->M; aw.Pdim = (int)cols;
-    aw.C = dW; aw.part = (float *)(ws + l.w_part);
+    aw.Qdim = cfg->K; aw.Kdim = l.terms * cfg->M; aw.Pdim = (int)cols;
+    aw.C = dW; aw.part = l.plan.w.splits > 1 ? (float *)(ws + l.w_part) : nullptr;
     if (dx || dW) {
         ProfScope ps("linear_backward", s);
         auto launch = bf ? launch_linear_backward_bf16 : launch_linear_backward_f32;
         if ((st = status_of(launch(l.plan, dx ? &ax : nullptr, dW ? &aw : nullptr, s)))) return st;
     }
     LinearJoin j{};
-    auto sum = [&](const LinearArgs &a, int splits) {
-        const int64_t elements = a.Qdim * a.Pdim;
+    auto sum = [&](const LinearArgs &a, int64_t rows, int splits) {
+        const int64_t elements = rows * a.Pdim;
         return LinearSum{a.part, a.C, elements, splits, (int)ceil_div(elements, kJoinThreads * (bf ? 8 : 4))};
     };
-    if (dx && l.plan.x.splits > 1) j.dx = sum(ax, l.plan.x.splits);
-    if (dW && l.plan.w.splits > 1) j.dW = sum(aw, l.plan.w.splits);
+    if (dx && l.x_parts > 1) j.dx = sum(ax, cfg->M, l.x_parts);
+    if (dW && l.plan.w.splits > 1) j.dW = sum(aw, cfg->K, l.plan.w.splits);
     if (!j.dx.blocks && !j.dW.blocks && !db) return SW_OK;
     ProfScope ps("linear_join", s);
     j.db_part = (const float *)(ws + l.db_part); j.db = db;

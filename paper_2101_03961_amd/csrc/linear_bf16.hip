@@ -87,7 +87,7 @@ __device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const Linea
             }
             if (row >= rows || !in) continue;
             const int64_t q = q0 + row;
-            if (t.cut.splits > 1) {
+            if (a.part) {
                 linear_store_part<8, GATED>(a, at.split, q, p, v, lin);
             } else if (KIND == LINEAR_FWD) {
                 float r8[8];

@@ -138,7 +138,7 @@ __device__ __forceinline__ void linear_f32_tile(const LinearArgs &a, const Linea
             v[m] = total[4 * g + m];
             if (GATED) lin[m] = total[8 + (4 * g + m) % 8];
         }
-        if (t.cut.splits > 1) {
+        if (a.part) {
             linear_store_part<4, GATED>(a, at.split, q, p, v, lin);
         } else if (KIND == LINEAR_FWD) {
             linear_emit<float, ACT>(a, q, p, v, lin);

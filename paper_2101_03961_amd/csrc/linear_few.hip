@@ -156,7 +156,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_few_kernel(LinearArg
                     if (GATED) lin[j] += from[kCols / 2 + j];
                 }
             }
-            if (cut.splits > 1) linear_store_part<n, GATED>(a, split, q, p, v, lin);
+            if (a.part) linear_store_part<n, GATED>(a, split, q, p, v, lin);
             else linear_emit<T, ACT>(a, q, p, v, lin);
         }
     }

@@ -187,6 +187,47 @@ def test_linear_parts_that_may_be_left_out(dtype):
         op.forward(dev["x"].double(), dev["W"])
 
 
+@pytest.mark.parametrize("act", ["gelu", "geglu"])
+@pytest.mark.parametrize("M,K,N", [(1, 8, 8), (1, 64, 128), (2, 768, 64), (5, 120, 280), (16, 72, 264), (33, 1000, 40),
+                                   (64, 64, 520), (100, 264, 136), (129, 40, 72), (255, 136, 8), (256, 520, 264)])
+def test_linear_gradients_of_few_rows_round_once(M, K, N, act):
+    """Up to 256 rows the products take dz in two bf16 terms: the second is the rest of the first's rounding (at most 2^-8 of
+    dz), rounded to 2^-8 of itself: dz is off by 2^-16.  (One term, off by 2^-8, would pass none of these bounds: where the
+    products cancel, or at one row, it is as large as the gradient's own rounding, or larger.)"""
+    rate, seed = 0.25, 77 + M
+    ref, dev = linear_case(M, K, N, act, "bf16", seed=M + K)
+    op = SwitchLinear(M, K, N, act, rate, seed, "bf16", DEV, train=True)
+    op.forward(dev["x"], dev["W"], dev["bias"])
+    for t in (op.dx, op.dW, op.db):
+        t.fill_(float("nan"))
+    op.workspace.fill_(255)
+    g = {k: v.clone() for k, v in op.backward(dev["dy"], dev["x"], dev["W"]).items()}
+    z = op.z.cpu().double()
+    dy = ref["dy"] * keep_factor(M * N, rate, seed).reshape(M, N)
+    dz = dz64(act, z, dy)
+    fit = 4e-7 * (torch.cat((dy * z.chunk(2, 1)[1], dy * z.chunk(2, 1)[0]), 1).abs() if act == "geglu" else dy.abs())
+    edz = dz.abs() * (2.0 ** -16 + 8 * U32) + fit * (1 + z.abs())
+    u = U["bf16"]
+    for name, a, b, ea, n in (("dx", dz, ref["W"].t(), edz @ ref["W"].abs().t(), 2 * dz.shape[1]),
+                              ("dW", ref["x"].t(), dz, ref["x"].abs().t() @ edz, 2 * M)):
+        want = a @ b
+        e = ea + (n + 2) * U32 * (a.abs() @ b.abs())
+        close(name, g[name], want, u * (want.abs() + e) + e, (math.sqrt(n) + 16) * U32 + u + 2.0 ** -15)
+    for name in ("dx", "dW", "db"):
+        out = torch.full_like(g[name], float("nan"))
+        sw.switch_linear_backward(op.cfg, dev["dy"], dev["x"] if name == "dW" else None, dev["W"] if name == "dx" else None,
+                                  op.z, *[out if k == name else None for k in ("dx", "dW", "db")], op.workspace,
+                                  op.workspace_bytes)
+        assert torch.equal(out, g[name]), name
+    # an infinity in x: its row of dW infinite, with dz's signs, and the other rows as they were
+    x, j = dev["x"].clone(), K // 2
+    x[M // 2, j] = float("inf")
+    dW = op.backward(dev["dy"], x, dev["W"])["dW"].cpu().double()
+    others, kept = torch.arange(K) != j, dz[M // 2] != 0
+    assert torch.equal(dW[others], g["dW"].cpu().double()[others])
+    assert torch.equal(dW[j][kept], dz[M // 2][kept].sign() * math.inf)
+
+
 def test_linear_without_rows():
     op = SwitchLinear(0, 64, 128, "gelu", 0.1, 3, "bf16", DEV, train=True)
     for t in (op.dW, op.db):
