@@ -12,7 +12,7 @@ namespace sw {
 
 // dz without the dropout's scale (so that, where act' is 0 or 1, it is dy or zero and loses nothing in bf16) and sums of its
 // rows.  A lane takes a chunk of columns, 16 bytes, of the gate and of the linear part; `lanes` lanes of a block share a row
-// and each handles kDzSteps rows, 256 / lanes apart.  Bound by its traffic.
+// and each handles `steps` rows, 256 / lanes apart.  Bound by its traffic.
 //
 // GELU's dz has more digits than bf16.  Its rounding adds as much error to a gradient as the gradient's own (together sqrt(2)
 // of one) where many values average it; over few rows a gradient hangs on few of them, and the two came to 1.5 to 2.1 of one
@@ -20,8 +20,8 @@ namespace sw {
 // sum of two bf16 terms, 16 digits, the second M rows below the first; the products, which W and dW bind there and not
 // their operations, take 2 M rows: dx's of both terms are added up as parts of k are, dW's k runs over both terms, over x
 // twice.  One term / two, us, 4096 -> 2 x 10240 gated: 16 rows 113 / 116, 256 rows 169 / 196, 1024 rows (were they to have two)
-// 315 / 554; 768 -> 2 x 2048: 1 row 12.5 / 14.0, 256 rows 29 / 35.
-constexpr int kDzSteps = 8, kTermRows = 256, kCopyBlocks = 512;
+// 315 / 554; 768 -> 2 x 2048: 1 row 12.5 / 14.0, 256 rows 29 / 35 (each at eight rows of a lane).
+constexpr int kTermRows = 256, kCopyBlocks = 512;
 static int linear_terms(const switch_linear_config *cfg) {
     const bool gelu = cfg->activation == SW_ACT_GELU || cfg->activation == SW_ACT_GEGLU;
     return cfg->act_dtype == SW_BF16 && gelu && cfg->M <= kTermRows ? 2 : 1;
@@ -36,7 +36,7 @@ struct DzArgs {
     int y_blocks;
     float *part;                   // [row blocks][columns of W], or nullptr
     int64_t M;
-    int N, act, lanes;
+    int N, act, lanes, steps;
     Drop drop;
 };
 
@@ -67,12 +67,12 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
         return;
     }
     const int p = (blockIdx.y * a.lanes + tid % a.lanes) * n;
-    const int64_t q0 = (int64_t)blockIdx.x * (lines * kDzSteps) + line;
+    const int64_t q0 = (int64_t)blockIdx.x * (lines * a.steps) + line;
     const int64_t Nz = NP * (int64_t)a.N;
     float sum[NP][n] = {};
     if (p < a.N)
 #pragma unroll 2
-        for (int i = 0; i < kDzSteps; ++i) {
+        for (int i = 0; i < a.steps; ++i) {
             const int64_t q = q0 + (int64_t)i * lines;
             if (q >= a.M) break;
             const int64_t at = q * a.N + p, zat = q * Nz + p;
@@ -330,7 +330,7 @@ struct LinearLayout {
     bool own_dz;                   // dz is not dy itself
     int terms;                     // of dz
     int x_parts;                   // sums of y or dx: parts of k, each of every term
-    int lanes;                     // of linear_dz_kernel
+    int lanes, steps;              // of linear_dz_kernel
     int64_t db_parts;
     LinearPlan plan;
 };
@@ -345,7 +345,11 @@ static LinearLayout linear_layout(const switch_linear_config *cfg, bool backward
         const int64_t chunks = cfg->N * elt / 16;
         l.lanes = 1;
         while (l.lanes < 32 && l.lanes < chunks) l.lanes *= 2;
-        l.db_parts = ceil_div(cfg->M, 256 / l.lanes * kDzSteps);
+        // rows of a lane: eight, fewer while the blocks are fewer than the CUs (a whole backward pass, gated, eight / so:
+        // 256 rows 120 -> 2 x 280: 33.8 / 15.5 us, 768 -> 2 x 2048: 35.2 / 26.5; 64 rows 4096 -> 2 x 10240: 158 / 148)
+        l.steps = 8;
+        while (l.steps > 1 && ceil_div(cfg->M, 256 / l.lanes * l.steps) * ceil_div(chunks, l.lanes) < kCUs) l.steps /= 2;
+        l.db_parts = ceil_div(cfg->M, 256 / l.lanes * l.steps);
         l.terms = linear_terms(cfg);
         l.dz = take(l.own_dz ? (size_t)l.terms * cfg->M * cols * elt : 0);
         l.x_twice = take(l.terms > 1 ? (size_t)2 * cfg->M * cfg->K * elt : 0);
@@ -437,7 +441,7 @@ int switch_linear_backward(const switch_linear_config *cfg, const void *dy, cons
         a.dy = dy; a.z = z;
         a.dz = l.own_dz && (dx || dW) ? ws + l.dz : nullptr;
         a.part = db ? (float *)(ws + l.db_part) : nullptr;
-        a.M = cfg->M; a.N = (int)cfg->N; a.act = cfg->activation; a.lanes = l.lanes;
+        a.M = cfg->M; a.N = (int)cfg->N; a.act = cfg->activation; a.lanes = l.lanes; a.steps = l.steps;
         a.drop = drop;
         a.y_blocks = (int)ceil_div(cfg->N, l.lanes * (bf ? 8 : 4));
         dim3 grid((unsigned)l.db_parts, (unsigned)a.y_blocks);
