@@ -243,8 +243,10 @@ int switch_forward_static(const switch_config *cfg, const void *x, const float *
  * (several choices per token, padded batches) needs the balance loss by itself.
  */
 
-/* Activation of switch_linear.  SW_ACT_GELU: u Phi(u), exact.  SW_ACT_GEGLU: GELU(u) * v with W
- * [K, 2 N] and bias [2 N], the N gate columns u first and the N linear columns v after them. */
+/* Activation of switch_linear.  SW_ACT_GELU: u Phi(u), Phi the normal distribution function (off by less than 4e-7
+ * of its value with SW_F32 and 1e-5 with SW_BF16, in the tail too, down to Phi(u) = 1e-37; less may be 0).
+ * SW_ACT_GEGLU: GELU(u) * v with W [K, 2 N] and bias [2 N], the N gate columns u first and the N linear columns v after
+ * them. */
 typedef enum { SW_ACT_NONE = 0, SW_ACT_RELU = 1, SW_ACT_GELU = 2, SW_ACT_GEGLU = 3 } sw_activation;
 
 typedef struct {

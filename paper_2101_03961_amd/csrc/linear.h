@@ -125,11 +125,11 @@ __device__ __forceinline__ void linear_init_q(OQ &oq, const LinearArgs &a, const
 
 // ---- epilogue -----------------------------------------------------------------------------------
 // act of a value, or of a gate and a linear part
-__device__ __forceinline__ float linear_act(int act, float u, float v) {
+template <typename T> __device__ __forceinline__ float linear_act(int act, float u, float v) {
     switch (act) {
     case SW_ACT_RELU: return fmaxf(u, 0.f);
-    case SW_ACT_GELU: return u * normal_of(u).cdf;
-    case SW_ACT_GEGLU: return u * normal_of(u).cdf * v;
+    case SW_ACT_GELU: return u * normal_at<T>(u).cdf;
+    case SW_ACT_GEGLU: return u * normal_at<T>(u).cdf * v;
     default: return u;
     }
 }
@@ -169,7 +169,7 @@ __device__ __forceinline__ void linear_emit(const LinearArgs &a, const LinearCol
         if (GATED) Row16<T>::store(a.z, zat + a.Pdim, lin);
     }
 #pragma unroll
-    for (int m = 0; m < n; ++m) v[m] = linear_act(ACT, v[m], GATED ? lin[m] : 0.f);
+    for (int m = 0; m < n; ++m) v[m] = linear_act<T>(ACT, v[m], GATED ? lin[m] : 0.f);
     if (a.drop.on) {
         drop_apply<n>(a.drop, (uint64_t)out, v);
 #pragma unroll

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
             } else if (a.act != SW_ACT_NONE) {
 #pragma unroll
                 for (int m = 0; m < n; ++m) {
-                    const NormalOf no = normal_of(u[m]);
+                    const NormalOf no = normal_at<T>(u[m]);
                     if (GATED) {
                         const float linear = v[m];
                         v[m] = g[m] * u[m] * no.cdf;
