@@ -271,7 +271,8 @@ int switch_linear_workspace_size(const switch_linear_config *cfg, int backward, 
  * One product with its epilogue:
  *   z = x W + bias        [M, N], for SW_ACT_GEGLU [M, 2 N]
  *   y = residual + dropout(act(z))
- * Products are summed in fp32, the epilogue is fp32 throughout; y and z are rounded once.  The
+ * Products are summed in fp32, the epilogue is fp32 throughout; y and z are rounded once.  A z that is NaN gives
+ * NaN with every activation, unless dropout makes it zero.  The
  * dropout mask is switch_dropout's for the same rate and seed and a tensor of M * N elements.
  * z, where asked for, is what switch_linear_backward needs; nothing else is kept.  residual and y
  * may be the same tensor; other tensors must not overlap an output.  M = 0: nothing is done (pointers may be NULL).
@@ -287,7 +288,7 @@ int switch_linear(const switch_linear_config *cfg,
 
 /*
  * Gradients of L = <dy, y>:  dz = act'(z) * dropout(dy),  dx = dz W^T,  dW = x^T dz,
- * db = sum of dz's rows (ReLU'(0) = 0); the residual's gradient is dy itself.  Each of dx, dW, db may
+ * db = sum of dz's rows (ReLU'(0) = 0, ReLU'(NaN) = NaN); the residual's gradient is dy itself.  Each of dx, dW, db may
  * be NULL, not all.  z: from switch_linear with the same cfg; not read (may be NULL) for
  * SW_ACT_NONE.  W is read only for dx, x only for dW; the other may be NULL.  With SW_BF16, SW_ACT_GELU
  * and SW_ACT_GEGLU round dz for the two products (db sums it in fp32): to bf16, or, up to 256 rows, to

@@ -127,7 +127,7 @@ __device__ __forceinline__ void linear_init_q(OQ &oq, const LinearArgs &a, const
 // act of a value, or of a gate and a linear part
 template <typename T> __device__ __forceinline__ float linear_act(int act, float u, float v) {
     switch (act) {
-    case SW_ACT_RELU: return fmaxf(u, 0.f);
+    case SW_ACT_RELU: return __builtin_elementwise_maximum(u, 0.f);   // (NaN stays NaN)
     case SW_ACT_GELU: return u * normal_at<T>(u).cdf;
     case SW_ACT_GEGLU: return u * normal_at<T>(u).cdf * v;
     default: return u;

@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(DzArgs a) {
             if (a.drop.on) drop_apply<n>(a.drop, (uint64_t)at, g);
             if (a.act == SW_ACT_RELU) {
 #pragma unroll
-                for (int m = 0; m < n; ++m) g[m] = u[m] > 0.f ? g[m] : 0.f;
+                for (int m = 0; m < n; ++m) g[m] = u[m] <= 0.f ? 0.f : u[m] > 0.f ? g[m] : u[m];   // (NaN stays NaN)
             } else if (a.act != SW_ACT_NONE) {
 #pragma unroll
                 for (int m = 0; m < n; ++m) {

@@ -32,8 +32,9 @@ __device__ __forceinline__ NormalOf normal_of(float u) {
 // a linear part of any size, is as good as the rest (the fit above is off by 5e-5 of Phi at u = -3 and 4e-3 at -6).
 // Phi(-|u|) = t poly(t) exp(-u^2 / 2), t = 1 / (1 + q |u|): t poly(t) was fitted to erfcx(|u| / sqrt 2) / 2 on 0 .. 13.4, where
 // Phi leaves the normal numbers, by least squares with weights raised where the relative error was largest; with its
-// rounded coefficients it is off by 5.4e-8.  fp32: a refined quotient and u^2 in two terms, off by less than 6 half
-// steps; bf16: the quotient within 1 ulp and the exponent's rounding, 8e-6 at u = -12, far inside the store's.
+// rounded coefficients it is off by 5.4e-8.  fp32: a refined quotient and u^2 in two terms, u Phi(u) measured to
+// be off by up to 6.1 half steps; bf16: the quotient within 1 ulp and the exponent's rounding, 8e-6 at u = -12, far inside the
+// store's.
 template <typename T> __device__ __forceinline__ NormalOf normal_at(float u) {
     constexpr float q = 0.339411259f, half_log2e = -0.72134752f;
     const float v = sizeof(T) == 4 ? fminf(fabsf(u), 16.f) : fabsf(u);   // (from 13.4 on all is 0 or 1)

@@ -14,7 +14,7 @@ import pytest
 import torch
 
 from paper_2101_03961_amd.layer import SwitchLinear
-from test_operators_gpu import DEV, DT, U, U32, phi
+from test_operators_gpu import ACTS, DEV, DT, U, U32, phi
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +72,45 @@ def test_gelu_value_by_value(act, M, N, dtype):
         want = g * u64 * cdf
         ok = (dx[:, N:] - want).abs() <= (half * (1 + own) + own) * want.abs()
         assert ok.all(), (u64[~ok][:4], dx[:, N:][~ok][:4], want[~ok][:4])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(48, 72, 264), (300, 72, 264), (48, 1032, 1032), (70, 1032, 520)])
+@pytest.mark.parametrize("act", ACTS)
+def test_nan_and_infinity_of_pre_activations(act, M, K, N, dtype):
+    """A value that is no number stays none through every activation, in y and in the gradients; beside its row and
+    column the same bits as without it.  An infinite pre-activation has its limit."""
+    gen = torch.Generator().manual_seed(M + N)
+    cols = N * (2 if act == "geglu" else 1)
+    normal = lambda *s: torch.randn(s, generator=gen).to(DT[dtype]).to(DEV)
+    x, W, dy = normal(M, K), normal(K, cols) * K ** -0.5, normal(M, N)
+    bias = torch.randn(cols, generator=gen).to(DEV)
+    op = SwitchLinear(M, K, N, act, 0.0, 0, dtype, DEV, train=True)
+    y = op.forward(x, W, bias).clone()
+    grads = {k: t.clone() for k, t in op.backward(dy, x, W).items()}
+    z = None if op.z is None else op.z.clone()
+    r, c = M // 2, N // 3
+    rows, at = torch.arange(M, device=DEV) != r, torch.arange(N, device=DEV) != c
+    bad = x.clone()
+    bad[r, 1] = float("nan")
+    out = op.forward(bad, W, bias)
+    assert torch.isnan(out[r]).all() and torch.equal(out[rows], y[rows])
+    b = bias.clone()
+    b[c] = float("nan")
+    out = op.forward(x, W, b)
+    assert torch.isnan(out[:, c]).all() and torch.equal(out[:, at], y[:, at])
+    b[c] = float("inf")
+    if act != "geglu":   # (there: infinity times a linear part)
+        assert (op.forward(x, W, b)[:, c] == float("inf")).all()
+    b[c] = -float("inf")
+    if act in ("none", "relu"):
+        assert (op.forward(x, W, b)[:, c] == (0.0 if act == "relu" else -float("inf"))).all()
+    if act == "none":
+        return
+    op.z.copy_(z)
+    op.z[r, c] = float("nan")
+    got = op.backward(dy, x, W)
+    assert torch.isnan(got["dx"][r]).all() and torch.equal(got["dx"][rows], grads["dx"][rows])
+    assert torch.isnan(got["dW"][:, c]).all() and torch.isnan(got["db"][c])
+    others = torch.arange(cols, device=DEV) % N != c
+    assert torch.equal(got["dW"][:, others], grads["dW"][:, others]) and torch.equal(got["db"][others], grads["db"][others])
