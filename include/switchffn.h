@@ -257,9 +257,14 @@ typedef struct {
     int32_t act_dtype;       /* sw_dtype of x, W, residual, y, z, dy, dx, dW          */
     int32_t activation;      /* sw_activation                                         */
     float dropout;           /* rate in [0, 1), rounded down to a multiple of 2^-16; 0: off */
-    int32_t flags;           /* 0                                                     */
+    int32_t flags;           /* 0, or SW_FLAG_DZ_TWO_TERMS; other bits are refused with SW_ERR_VALUE */
     uint64_t seed;           /* of the dropout; the same in forward and backward      */
 } switch_linear_config;
+
+/* Keep dz of SW_ACT_GELU and SW_ACT_GEGLU to 16 bits, not 8, for the two products of the backward pass with SW_BF16,
+ * whatever the number of rows (see switch_linear_backward): dx and dW are then off by their own rounding alone, and the
+ * products take twice as long.  No effect on other activations, on SW_F32 and on the forward pass. */
+#define SW_FLAG_DZ_TWO_TERMS 2
 
 /* Bytes of device workspace of switch_linear (backward = 0) or of switch_linear_backward
  * (backward = 1); may be 0.  Host only.  The workspace must be 256-byte aligned.  It holds nothing
@@ -291,9 +296,9 @@ int switch_linear(const switch_linear_config *cfg,
  * db = sum of dz's rows (ReLU'(0) = 0, ReLU'(NaN) = NaN); the residual's gradient is dy itself.  Each of dx, dW, db may
  * be NULL, not all.  z: from switch_linear with the same cfg; not read (may be NULL) for
  * SW_ACT_NONE.  W is read only for dx, x only for dW; the other may be NULL.  With SW_BF16, SW_ACT_GELU
- * and SW_ACT_GEGLU round dz for the two products (db sums it in fp32): to bf16, or, up to 256 rows, to
- * the sum of two bf16 terms (an infinite weight may then give NaN in its column of dx); the others need
- * no rounding: the dropout scale is applied to the sums.  No output may overlap an input.  M = 0: dW
+ * and SW_ACT_GEGLU round dz for the two products (db sums it in fp32): to bf16, or, up to 256 rows and with
+ * SW_FLAG_DZ_TWO_TERMS, to the sum of two bf16 terms (an infinite weight may then give NaN in its column of dx); the
+ * others need no rounding: the dropout scale is applied to the sums.  No output may overlap an input.  M = 0: dW
  * and db are zeros.
  */
 int switch_linear_backward(const switch_linear_config *cfg,

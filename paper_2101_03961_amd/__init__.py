@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     SW_F32,
     SW_FFN_GEGLU,
     SW_FFN_RELU,
+    SW_FLAG_DZ_TWO_TERMS,
     SW_FLAG_FUSED_DISPATCH,
     SwitchBalanceConfig,
     SwitchConfig,

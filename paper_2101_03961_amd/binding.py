@@ -11,6 +11,7 @@ _LIB_PATH = os.path.join(HERE, "libswitchffn.so")
 SW_F32, SW_BF16 = 0, 1
 SW_FFN_RELU, SW_FFN_GEGLU = 0, 1
 SW_FLAG_FUSED_DISPATCH = 1
+SW_FLAG_DZ_TWO_TERMS = 2
 SW_ACT_NONE, SW_ACT_RELU, SW_ACT_GELU, SW_ACT_GEGLU = 0, 1, 2, 3
 
 

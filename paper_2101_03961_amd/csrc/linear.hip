@@ -24,7 +24,7 @@ namespace sw {
 constexpr int kTermRows = 256, kCopyBlocks = 512;
 static int linear_terms(const switch_linear_config *cfg) {
     const bool gelu = cfg->activation == SW_ACT_GELU || cfg->activation == SW_ACT_GEGLU;
-    return cfg->act_dtype == SW_BF16 && gelu && cfg->M <= kTermRows ? 2 : 1;
+    return cfg->act_dtype == SW_BF16 && gelu && (cfg->M <= kTermRows || cfg->flags & SW_FLAG_DZ_TWO_TERMS) ? 2 : 1;
 }
 struct DzArgs {
     const void *dy, *z;
@@ -321,7 +321,7 @@ static int check_linear(const switch_linear_config *cfg) {
     if (cfg->K * elt % 16 || cfg->N * elt % 16) return SW_ERR_SHAPE;
     if (cfg->K * linear_columns(cfg) * elt >= (int64_t)1 << 31) return SW_ERR_SHAPE;
     if (!drop_rate_ok(cfg->dropout)) return SW_ERR_VALUE;
-    if (cfg->flags) return SW_ERR_VALUE;
+    if (cfg->flags & ~SW_FLAG_DZ_TWO_TERMS) return SW_ERR_VALUE;
     return SW_OK;
 }
 

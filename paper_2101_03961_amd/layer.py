@@ -120,18 +120,20 @@ def _device(device) -> torch.device:
 class SwitchLinear:
     """y = residual + dropout(act(x W + bias)) and its gradients (switch_linear).
 
-    `train`: also keep z for the backward pass and allocate the gradients.  Outputs are the
-    object's own buffers, overwritten by the next call."""
+    `train`: also keep z for the backward pass and allocate the gradients.  `dz_two_terms`: 16 bits of GELU's
+    dz for bf16 gradients, at any number of rows (SW_FLAG_DZ_TWO_TERMS).  Outputs are the object's own buffers,
+    overwritten by the next call."""
 
     ACTIVATIONS = {"none": B.SW_ACT_NONE, "relu": B.SW_ACT_RELU, "gelu": B.SW_ACT_GELU,
                    "geglu": B.SW_ACT_GEGLU}
 
     def __init__(self, M: int, K: int, N: int, activation: str = "none", dropout: float = 0.0, seed: int = 0,
-                 dtype: str = "bf16", device: str = "cuda:0", train: bool = False):
+                 dtype: str = "bf16", device: str = "cuda:0", train: bool = False, dz_two_terms: bool = False):
         if not torch.cuda.is_available():
             raise RuntimeError("SwitchLinear needs a GPU: the product runs only in the HIP library")
         self.cfg = B.SwitchLinearConfig(M, K, N, B.SW_BF16 if dtype == "bf16" else B.SW_F32,
-                                        self.ACTIVATIONS[activation], float(dropout), 0, int(seed))
+                                        self.ACTIVATIONS[activation], float(dropout),
+                                        B.SW_FLAG_DZ_TWO_TERMS if dz_two_terms else 0, int(seed))
         self.columns = N * (2 if activation == "geglu" else 1)   # of W
         self.device = _device(device)
         self.act = torch.bfloat16 if dtype == "bf16" else torch.float32

@@ -107,3 +107,38 @@ def test_large_tiles_backward(M, K, N, act, rate, dx_parts, dW_parts):
         e = e + (n + 2) * U32 * (a.abs() @ b.abs())
         close(name, got[name], want, u * (want.abs() + e) + e, (math.sqrt(n) + 16) * U32 + u + rounded)
         assert (big[name][:300] == 3.0).all() and (big[name][300 + got[name].shape[0]:] == 3.0).all(), name
+
+
+@pytest.mark.parametrize("act", ["gelu", "geglu"])
+@pytest.mark.parametrize("M,K,N", [(257, 264, 136), (1000, 72, 520), (2823, 2984, 728), (8929, 744, 512)])
+def test_two_terms_of_dz_on_request(M, K, N, act):
+    """dz in two bf16 terms is off by 2^-16 (the second, at most 2^-8 of dz, is rounded to 2^-8 of itself): the gradients
+    are off by their own rounding.  In small and in large tiles."""
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    cols, seed = N * (2 if act == "geglu" else 1), M
+    x, W = operand(gen, M, K).bfloat16(), operand(gen, K, cols).mul_(K ** -0.5).bfloat16()
+    dy, z = operand(gen, M, N).bfloat16(), operand(gen, M, cols).bfloat16()
+    op = SwitchLinear(M, K, N, act, 0.1, seed, "bf16", DEV, train=True, dz_two_terms=True)
+    op.z.copy_(z)
+    op.workspace.fill_(255)
+    for t in (op.dx, op.dW, op.db):
+        t.fill_(float("nan"))
+    got = op.backward(dy, x, W)
+    g = dy.double() * keep_factor(M * N, 0.1, seed).reshape(M, N).to(DEV)
+    dz = dz64(act, z.double(), g)
+    lin = g if act == "gelu" else torch.cat((g * z.double().chunk(2, 1)[1], g * z.double().chunk(2, 1)[0]), 1)
+    edz = dz.abs() * (2.0 ** -16 + 8 * U32) + 4e-7 * lin.abs() * (1 + z.double().abs())
+    for name, a, b, e, n in (("dx", dz, W.double().t().contiguous(), edz @ W.double().abs().t().contiguous(), 2 * cols),
+                             ("dW", x.double().t().contiguous(), dz, x.double().abs().t().contiguous() @ edz, 2 * M)):
+        want = a @ b
+        e = e + (n + 2) * U32 * (a.abs() @ b.abs())
+        close(name, got[name], want, u * (want.abs() + e) + e, (math.sqrt(n) + 16) * U32 + u + 2.0 ** -15)
+        # an evenly distributed rounding, 2^-8 / sqrt(3) of the bottom of a value's binade, is 0.426 of 2^-8 in the norm of normally
+        # distributed values of any variance (one term's and the gradient's own together: sqrt(2) times that)
+        rms = float(torch.linalg.norm(got[name].double() - want) / torch.linalg.norm(want))
+        assert rms <= 0.45 * u, (name, rms)
+    dx, dW, db = (t.clone() for t in (got["dx"], got["dW"], got["db"]))
+    one = SwitchLinear(M, K, N, act, 0.1, seed, "bf16", DEV, train=True)
+    one.z.copy_(z)
+    assert torch.equal(one.backward(dy, x, W)["db"], db)
+    assert not torch.equal(one.dx, dx) and not torch.equal(one.dW, dW)

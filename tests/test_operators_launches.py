@@ -51,3 +51,23 @@ def test_large_tiles_backward(record, M, K, N, act, dropout, dx_parts, dW_parts)
     cols = N * (2 if act == "geglu" else 1)
     blocks = -(-cols // 32) + dx_parts * -(-M * K // 8192) + dW_parts * -(-K * cols // 8192)
     assert launches[-1][1] == (blocks, 1, 1)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_two_terms_of_dz_on_request(record, act):
+    """Twice the rows in dx's products and twice the k in dW's, for GELU in bf16 only; other flags are refused."""
+    assert sw.SW_FLAG_DZ_TWO_TERMS == 2
+    M, K, N = 8192, 4096, 1024
+    one, two = (record("backward", M, K, N, act, flags=flags) for flags in (0, sw.SW_FLAG_DZ_TWO_TERMS))
+    assert one[0] == two[0] == 0
+    gelu = act in ("gelu", "geglu")
+    assert (two == one) == (not gelu)
+    if gelu:   # both terms' sums of dx, at least
+        assert two[1] >= one[1] + 2 * M * K * 4
+    assert record("backward", M, K, N, act, dtype=sw.SW_F32, flags=2) == record("backward", M, K, N, act, dtype=sw.SW_F32)
+    assert record("forward", M, K, N, act, flags=2) == record("forward", M, K, N, act)
+    for flags in (1, 3, 4, -1):
+        for what in ("forward", "backward"):
+            assert record(what, M, K, N, act, flags=flags)[0] == -3
+    # few rows have them anyway
+    assert record("backward", 256, K, N, act, flags=2) == record("backward", 256, K, N, act)
