@@ -16,11 +16,11 @@ namespace sw {
 //
 // GELU's dz has more digits than bf16.  Its rounding adds as much error to a gradient as the gradient's own (together sqrt(2)
 // of one) where many values average it; over few rows a gradient hangs on few of them, and the two came to 1.5 to 2.1 of one
-// (1 to 5 rows; at most 1.55 at 32, 1.48 at 128, 1.47 at 256 and 512).  So up to kTermRows rows dz is kept as the
-// sum of two bf16 terms, 16 digits, the second M rows below the first; the products, which W and dW bind there and not
-// their operations, take 2 M rows: dx's of both terms are added up as parts of k are, dW's k runs over both terms, over x
-// twice.  One term / two, us, 4096 -> 2 x 10240 gated: 16 rows 113 / 116, 256 rows 169 / 196, 1024 rows (were they to have two)
-// 315 / 554; 768 -> 2 x 2048: 1 row 12.5 / 14.0, 256 rows 29 / 35 (each at eight rows of a lane).
+// (1 to 5 rows; at most 1.55 at 32, 1.48 at 128, 1.47 at 256 and 512).  So up to kTermRows rows, and where a caller asks
+// for it, dz is kept as the sum of two bf16 terms, 16 digits, the second M rows below the first; the products, which W and dW
+// bind there and not their operations, take 2 M rows: dx's of both terms are added up as parts of k are, dW's k runs over both
+// terms, over x twice.  One term / two, us, 4096 -> 2 x 10240 gated: 16 rows 108 / 113, 64 rows 113 / 142, 256 rows 166 / 201,
+// 1024 rows 329 / 581, 8192 rows 2146 / 4419; 768 -> 2 x 2048: 1 row 13.6 / 14.9, 16 rows 17.4 / 22.4, 256 rows 22.0 / 26.4.
 constexpr int kTermRows = 256, kCopyBlocks = 512;
 static int linear_terms(const switch_linear_config *cfg) {
     const bool gelu = cfg->activation == SW_ACT_GELU || cfg->activation == SW_ACT_GEGLU;
