@@ -134,7 +134,10 @@ typedef struct {
  *     z = (idx ^ seed_lo) * 0x9E3779B1;  z ^= z >> 15;
  *     z = (z + seed_hi + s * 0x7F4A7C15) * 0x85EBCA77;  z ^= z >> 13;
  *     z *= 0xC2B2AE3D;  z ^= z >> 16;            (all arithmetic modulo 2^32)
- * with seed_lo / seed_hi the two halves of seed.
+ * with seed_lo / seed_hi the two halves of seed.  Seeds a and b with the same upper half draw the same
+ * values in another order (b at idx what a draws at idx ^ a_lo ^ b_lo): seeds that are counted up give masks that
+ * are permutations of one another.  Put counters through a 64-bit mixing function, so that both halves of every
+ * step's and every sublayer's seed differ (layer.py: mixed_seed).
  *   jitter  (s = 1, idx = t * d_model + k):  m = fma(2 eps, (z >> 8) * 2^-24, 1 - eps) in fp32
  *   dropout (s = 2):  hidden unit j of token t (the token -- not its slot) is element
  *           i = t * d_ff + j; it takes 16 bits of the z drawn for idx = i / 2 -- z & 0xFFFF if
@@ -258,7 +261,7 @@ typedef struct {
     int32_t activation;      /* sw_activation                                         */
     float dropout;           /* rate in [0, 1), rounded down to a multiple of 2^-16; 0: off */
     int32_t flags;           /* 0, or SW_FLAG_DZ_TWO_TERMS; other bits are refused with SW_ERR_VALUE */
-    uint64_t seed;           /* of the dropout; the same in forward and backward      */
+    uint64_t seed;           /* of the dropout; the same in forward and backward, well mixed ("Random draws") */
 } switch_linear_config;
 
 /* Keep dz of SW_ACT_GELU and SW_ACT_GEGLU to 16 bits, not 8, for the two products of the backward pass with SW_BF16,

@@ -4,7 +4,7 @@
 memory and streams are all torch is used for) and forwards every call to
 `switch_forward` / `switch_backward`; `SwitchLinear` and `SwitchBalanceLoss` do the same
 for the operators around the layer, `dropout` for the one without buffers.  They perform no
-arithmetic.
+arithmetic.  `mixed_seed` makes seeds for all of them.
 """
 from __future__ import annotations
 
@@ -13,6 +13,20 @@ from typing import Dict, Optional
 import torch
 
 from . import binding as B
+
+
+def mixed_seed(*counters: int) -> int:
+    """A 64-bit seed from counters such as (step, sublayer).  Seeds that are counted up themselves give masks that are
+    permutations of one another: the generator takes the lower half of a seed by exclusive or with the element.
+    (SplitMix64, Steele, Lea and Flood 2014.)"""
+    word = (1 << 64) - 1
+    z = len(counters)
+    for c in counters:
+        z = (z + int(c) + 0x9E3779B97F4A7C15) & word
+        z = ((z ^ z >> 30) * 0xBF58476D1CE4E5B9) & word
+        z = ((z ^ z >> 27) * 0x94D049BB133111EB) & word
+        z ^= z >> 31
+    return z
 
 
 class SwitchLayer:
@@ -50,7 +64,7 @@ class SwitchLayer:
         self.dx = self.dW_r = self.db_r = self.dW_in = self.dW_out = None
 
     def set_seed(self, seed: int) -> None:
-        """Seed of the training-time noise for the next forward + backward pair."""
+        """Seed of the training-time noise for the next forward + backward pair; see mixed_seed."""
         self.cfg.seed = int(seed)
 
     def _stream(self) -> int:
@@ -153,7 +167,7 @@ class SwitchLinear:
             self.db = torch.empty(self.columns, dtype=torch.float32, device=dev)
 
     def set_seed(self, seed: int) -> None:
-        """Seed of the dropout for the next forward + backward pair."""
+        """Seed of the dropout for the next forward + backward pair; see mixed_seed."""
         self.cfg.seed = int(seed)
 
     def _stream(self) -> int:
@@ -184,7 +198,8 @@ class SwitchLinear:
 
 
 def dropout(x, rate: float, seed: int, residual=None, out=None) -> torch.Tensor:
-    """residual + dropout(x) (switch_dropout); the gradient of x is the same call on that of the result."""
+    """residual + dropout(x) (switch_dropout); the gradient of x is the same call on that of the result.  Seeds of
+    other steps and sublayers: mixed_seed."""
     if x.dtype not in (torch.bfloat16, torch.float32) or x.device.type != "cuda":
         raise ValueError("x must be a bfloat16 or float32 tensor on a GPU, got %s on %s" % (x.dtype, x.device))
     shape = tuple(x.shape)
