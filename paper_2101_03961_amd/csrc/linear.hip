@@ -227,8 +227,9 @@ template <typename T> static hipError_t linear_finish(const LinearArgs &a, int s
 // Per kind of tile: k of a step; us of a step per block of a CU (of the blocks that share it, one after the other) and of
 // a step at least; us of a block's start and end, forward and backward (whose parts of dW are stored in fp32); blocks that a
 // CU holds.  Fitted to products of 4 to 64 steps and to backward passes with 1 to 48 parts of dW; us of dx and dW, as chosen
-// (tile, parts) / the best of all: 16384 x 768 x 2048 (256, 12) 119 / 119; 65536 x 2048 x 768 (256, 8) 461 / 461; 8192 x 2048 x 768
-// (256, 8) 75 / 67; 5000 x 520 x 1000 (128, 6) 27 / 27; 2048 x 4096 x 4096 (256, 1) 119 / 118; 30000 x 264 x 520 (128, 16) 48 / 46.
+// (tile, parts) / the best of all: 16384 x 768 x 2048 (256, 12) 119 / 119; 65536 x 2048 x 768 (256, 8) 461 / 461;
+// 8192 x 2048 x 768 (256, 8) 75 / 67; 5000 x 520 x 1000 (128, 6) 27 / 27; 2048 x 4096 x 4096 (256, 1) 119 / 118;
+// 30000 x 264 x 520 (128, 16) 48 / 46.
 struct LinearModel {
     int tile, bk;
     double step, least, once_fwd, once_bwd;

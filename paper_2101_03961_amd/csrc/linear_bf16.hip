@@ -2,11 +2,12 @@
 // time through LDS stages filled by direct loads.
 //
 // Large tiles, 256 x 256 in four waves, one block per CU, for products that fill the chip with them: bound by the matrix cores
-// under their own power (8192 x 8192 x 8192: 1320 - 1450 TFLOP/s; 8192 x 8192 x 4096 of zeros, which draw less, 1600 - 1780), and by a tile's start
-// and end, 10 us beside 1.45 us a step: at its end all CUs store at once.  (Persistent blocks of eight waves with the next tile's loads under way
-// during the epilogue: 65536 x 2048 x 768 205 us, the plain eight-wave kernel 202.  Tiles of 256 x 128, two blocks per CU, whose starts
-// and ends the other block covers, with 32 k a step to fit the LDS: 1.9 us for the products that take 1.45.)  Small tiles, 128 x 128, two blocks per CU,
-// where the large ones leave CUs idle.  linear.hip chooses.
+// under their own power (8192 x 8192 x 8192: 1320 - 1450 TFLOP/s; 8192 x 8192 x 4096 of zeros, which draw less,
+// 1600 - 1780), and by a tile's start and end, 10 us beside 1.45 us a step: at its end all CUs store at once.  (Persistent
+// blocks of eight waves with the next tile's loads under way during the epilogue: 65536 x 2048 x 768 205 us, the plain
+// eight-wave kernel 202.  Tiles of 256 x 128, two blocks per CU, whose starts and ends the other block covers, with 32 k a
+// step to fit the LDS: 1.9 us for the products that take 1.45.)  Small tiles, 128 x 128, two blocks per CU, where the large
+// ones leave CUs idle.  linear.hip chooses.
 #include "linear.h"
 #include "rows_operands.h"
 
@@ -38,8 +39,8 @@ template <int IP, int WP, int NW> struct GatedTrans : RowsTrans<32 * IP * WP, NW
 // Epilogue of a wave: 16 rows at a time through 2 KB IP of LDS of its own, as fp32, so that a lane has eight consecutive
 // columns (of the gate and the linear part) and rows leave in whole segments.  The 16-byte chunks of a row trade places by
 // the row, so that neither side has bank conflicts.
-template <int IP, int IQ, int WQ, LinearKind KIND, int ACT>
-__device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const LinearTiles &t, const LinearPlace &at,
+template <int IP, int IQ, LinearKind KIND, int ACT>
+__device__ __forceinline__ void linear_epilogue(const LinearArgs &a, const LinearPlace &at,
                                                 const f32x4 (&acc)[2 * IP][2 * IQ], char *turn, int lane, int wp, int wq) {
     static_assert(IP % 2 == 0, "whole groups of 16 chunks of a row");
     constexpr bool GATED = ACT == SW_ACT_GEGLU;
@@ -140,8 +141,8 @@ __device__ __forceinline__ void products4_load(f32x4 &c0, f32x4 &c1, f32x4 &c2, 
 
 // One large tile: four waves of 128 x 128, one per SIMD, whose fragments take a third less LDS traffic than those of eight
 // waves of 64 x 128 (1536 cycles of reads and fills per step, the products take 2048).  P goes through three stages of 32 KB, Q
-// through two.  In the middle of step kt a barrier ends the reads of its stages; Q's is filled with step kt + 2 in the second half
-// of the step, P's with step kt + 3 in the first half of the next one: a load and two reads per eight products throughout
+// through two.  In the middle of step kt a barrier ends the reads of its stages; Q's is filled with step kt + 2 in the second
+// half of the step, P's with step kt + 3 in the first half of the next one: a load and two reads per eight products throughout
 // (all 16 loads in the second half: dx of 8192 x 8192 x 4096 380 us, 374 so; of zeros 313 and 301).  The fragments of a half
 // step are read during the products of the half step before.
 template <LinearKind KIND, int ACT>
@@ -198,7 +199,8 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
     uint32_t sp = 0, sq = 0;   // stages of step kt
 #pragma nounroll
     for (int kt = 0; kt < nk; ++kt) {
-        const uint32_t sp1 = sp == 2 * kStageP ? 0 : sp + kStageP, sp2 = sp1 == 2 * kStageP ? 0 : sp1 + kStageP, sq1 = sq ^ kStageQ;
+        const uint32_t sp1 = sp == 2 * kStageP ? 0 : sp + kStageP, sp2 = sp1 == 2 * kStageP ? 0 : sp1 + kStageP;
+        const uint32_t sq1 = sq ^ kStageQ;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             op.reload_frag();
@@ -246,7 +248,7 @@ __device__ __forceinline__ void linear_large(const LinearArgs &a, const LinearTi
 #pragma unroll
         for (int j = 0; j < 2 * IQ; ++j) asm volatile("" : "+a"(acc[i][j]));
     __syncthreads();
-    linear_epilogue<IP, IQ, WQ, KIND, ACT>(a, t, at, acc, lds + wave * S::kTurn, lane, wp, wq);
+    linear_epilogue<IP, IQ, KIND, ACT>(a, at, acc, lds + wave * S::kTurn, lane, wp, wq);
 }
 
 template <int ACT>
@@ -319,7 +321,7 @@ __device__ __forceinline__ void linear_small(const LinearArgs &a, const LinearTi
         }
     }
     __syncthreads();
-    linear_epilogue<IP, IQ, WQ, KIND, ACT>(a, t, at, acc, lds + wave * S::kTurn, lane, wp, wq);
+    linear_epilogue<IP, IQ, KIND, ACT>(a, at, acc, lds + wave * S::kTurn, lane, wp, wq);
 }
 
 template <int ACT>

@@ -18,7 +18,7 @@ constexpr int kFewRows = 64, kFewWaves = 8;
 
 template <typename T> struct FewChunk;   // a lane's share of a chunk: W rows of 16 bytes, MFMA operands
 template <> struct FewChunk<bf16> {
-    static constexpr int kRows = 32, kLoads = 8, kOperands = 8;   // k rows, W loads per lane, MFMA per row block
+    static constexpr int kRows = 32, kLoads = 8;   // k rows, W loads per lane
     u32x4 w[kLoads];
     // k rows 8 g + i of chunk k
     __device__ __forceinline__ static int row(int g, int i) { return 8 * g + i; }
@@ -37,7 +37,7 @@ template <> struct FewChunk<bf16> {
     }
 };
 template <> struct FewChunk<float> {
-    static constexpr int kRows = 16, kLoads = 4, kOperands = 4;
+    static constexpr int kRows = 16, kLoads = 4;
     u32x4 w[kLoads];
     __device__ __forceinline__ static int row(int g, int i) { return 4 * g + i; }
     // (an MFMA takes one k of each lane group: 4 g + i of all g)
@@ -75,7 +75,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_few_kernel(LinearArg
     const int k0 = (int)(split * cut.split_k), kend = (int)min(a.Kdim, k0 + cut.split_k), K = (int)a.Kdim;
     // the lane's columns of W; rows past the last one lie past the descriptor
     const int col = GATED ? p0 + (c & 7) * n : p0 + c * n;
-    const auto wsrc = __builtin_amdgcn_make_buffer_rsrc((void *)a.P, 0, (int)((uint32_t)K * (uint32_t)a.ldp * sizeof(T)), 0x00020000);
+    const auto wsrc = __builtin_amdgcn_make_buffer_rsrc((void *)a.P, 0, (int)((uint32_t)K * (uint32_t)a.ldp * sizeof(T)),
+                                                        0x00020000);
     const i32x4 xsrc = make_rsrc(a.Q, (uint32_t)a.Qdim * (uint32_t)K * sizeof(T));
     const uint32_t wcol = col < a.Pdim ? (uint32_t)(GATED && c >= 8 ? a.Pdim + col : col) * sizeof(T) : kOobOffset;
     // x: load i of the wave is rows 2 (8 i + wave) + lane / 32, 512 bytes each; the 16-byte chunks of a row trade places by the
@@ -96,7 +97,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_few_kernel(LinearArg
 #pragma unroll
         for (int i = 0; i < Chunk::kLoads; ++i) {
             const uint32_t off = (uint32_t)(k + Chunk::row(g, i)) * (uint32_t)a.ldp * sizeof(T) + wcol;
-            ch.w[i] = __builtin_amdgcn_raw_buffer_load_b128(wsrc, (int)(first == kOobOffset ? kOobOffset : off), 0, STREAM ? 2 : 0);
+            ch.w[i] = __builtin_amdgcn_raw_buffer_load_b128(wsrc, (int)(first == kOobOffset ? kOobOffset : off), 0,
+                                                            STREAM ? 2 : 0);
         }
         const uint32_t to = lds0 + (uint32_t)(r % 3 * kStage);
 #pragma unroll
@@ -164,8 +166,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_few_kernel(LinearArg
 
 bool linear_few_rows(const switch_linear_config *cfg) { return cfg->M <= kFewRows; }
 
-// Parts of k that give every CU a block, as long as each wave has two chunks (us with 1, 4, 8, 16 parts: 48 x 10240 x 4096 74, 29,
-// 23, 32; 64 x 8192 x 1024 45, 19, 15, 15; 1 x 768 x 4096 6.5, 7.7, 9.1, 9.7; 1 x 4096 x 20480, 160 blocks without, 32, 34, 33, 38).
+// Parts of k that give every CU a block, as long as each wave has two chunks (us with 1, 4, 8, 16 parts: 48 x 10240 x 4096
+// 74, 29, 23, 32; 64 x 8192 x 1024 45, 19, 15, 15; 1 x 768 x 4096 6.5, 7.7, 9.1, 9.7; 1 x 4096 x 20480, 160 blocks without,
+// 32, 34, 33, 38).
 LinearCut linear_few_cut(const switch_linear_config *cfg) {
     const bool bf = cfg->act_dtype == SW_BF16;
     const int64_t tiles = ceil_div(linear_columns(cfg), bf ? 128 : 64), least = kFewWaves * (bf ? 32 : 16) * 2;
@@ -189,16 +192,17 @@ static hipError_t linear_few_launch(const LinearPlan &plan, const LinearArgs &a,
 }
 // A W of more than 32 MB streams past the caches (us, without / with: 48 x 10240 x 4096 24.8 / 24.0, 1 x 4096 x 20480 32.5 /
 // 31.6; but 64 x 8192 x 1024 14.4 / 15.3, 32 x 2048 x 768 8.7 / 10.0).
-template <typename T, int MT, int ACT> static hipError_t linear_few_rows(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
+template <typename T, int MT, int ACT>
+static hipError_t linear_few_caches(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
     return a.Kdim * a.ldp * (int64_t)sizeof(T) > 32 << 20 ? linear_few_launch<T, MT, ACT, true>(plan, a, s)
                                                           : linear_few_launch<T, MT, ACT, false>(plan, a, s);
 }
 template <typename T, int ACT> static hipError_t linear_few(const LinearPlan &plan, const LinearArgs &a, hipStream_t s) {
     switch (ceil_div(a.Qdim, 16)) {
-    case 1: return linear_few_rows<T, 1, ACT>(plan, a, s);
-    case 2: return linear_few_rows<T, 2, ACT>(plan, a, s);
-    case 3: return linear_few_rows<T, 3, ACT>(plan, a, s);
-    default: return linear_few_rows<T, 4, ACT>(plan, a, s);
+    case 1: return linear_few_caches<T, 1, ACT>(plan, a, s);
+    case 2: return linear_few_caches<T, 2, ACT>(plan, a, s);
+    case 3: return linear_few_caches<T, 3, ACT>(plan, a, s);
+    default: return linear_few_caches<T, 4, ACT>(plan, a, s);
     }
 }
 
