@@ -71,3 +71,16 @@ def test_two_terms_of_dz_on_request(record, act):
             assert record(what, M, K, N, act, flags=flags)[0] == -3
     # few rows have them anyway
     assert record("backward", 256, K, N, act, flags=2) == record("backward", 256, K, N, act)
+
+
+@pytest.mark.parametrize("act", ["none", "geglu"])
+@pytest.mark.parametrize("M,K,N,dtype", [(16, 8192, 256, sw.SW_BF16), (16, 8192, 256, sw.SW_F32), (100, 4096, 256, sw.SW_BF16)])
+def test_forward_refuses_a_workspace_that_is_too_small(record, M, K, N, dtype, act):
+    """Forward passes in parts of k need one: never followed, too small, none, and not on 256 bytes."""
+    at = 0x1000
+    status, need, launches = record("forward", M, K, N, act, dtype=dtype)
+    assert status == 0 and need > 0 and names(launches)[1:] == ["linear_finish"]
+    cfg = sw.SwitchLinearConfig(M, K, N, dtype, ACTS.index(act), 0.0, 0, 0)
+    assert sw.switch_linear_workspace_size(cfg, False) == need
+    for ws, size in ((at, need - 1), (at, 0), (None, need), (at + 16, need)):
+        assert sw.switch_linear(cfg, at, at, None, None, at, None, ws, size, check=False) == -5
